@@ -1,5 +1,5 @@
 """ctypes binding of ``libautopoiesis_eval.so``: the same names as the C ABI
-(``include/autopoiesis_eval.h``), argument marshalling only.  Every step of the
+(``include/autopoiesis_eval.h``, ``include/autopoiesis_attn.h``), argument marshalling only.  Every step of the
 evaluation runs in the library's HIP kernels; PyTorch is used by callers for device
 memory and streams.  There is no fallback: a missing library raises at load time.
 """
@@ -40,6 +40,28 @@ assert REPLICA_DTYPE.itemsize == 32 and METRICS_DTYPE.itemsize == 64 and MODEL_D
 
 class ApSlo(C.Structure):
     _fields_ = [("ttft_us", C.c_uint64), ("tpot_us", C.c_uint64), ("penalty_us", C.c_uint64)]
+
+
+AP_BF16, AP_FP16 = 0, 1
+
+
+class ApKvCache(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "bits", "n_pages", "page_size", "kv_heads", "head_dim")] + \
+               [(n, C.c_void_p) for n in ("k", "v", "k_pairs", "v_pairs")] + \
+               [(n, C.c_int64) for n in ("page_stride", "head_stride", "slot_stride", "pair_page_stride", "pair_head_stride", "pair_slot_stride")]
+
+
+class ApSeqBatch(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("n_seqs", "n_tokens", "max_new", "max_kv", "table_width")] + \
+               [(n, C.c_void_p) for n in ("new_first", "kv_len", "page_table")] + [("table_stride", C.c_int64)]
+
+
+class ApRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class ApRotation(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("n_positions", C.c_uint32), ("rot_dim", C.c_uint32), ("neighbours", C.c_uint32)]
 
 
 class ApError(RuntimeError):
@@ -106,6 +128,15 @@ def lib() -> C.CDLL:
         L.ap_hist_bin.restype = C.c_uint32
         L.ap_hist_lower.argtypes = [C.c_uint32]
         L.ap_hist_lower.restype = C.c_uint64
+        cache, batch, rows, rotation = (C.POINTER(t) for t in (ApKvCache, ApSeqBatch, ApRows, ApRotation))
+        L.ap_kv_append.argtypes = [cache, batch, rows, rows, rotation, rows, rows, C.c_uint32, C.c_void_p]
+        L.ap_kv_append.restype = C.c_int
+        L.ap_kv_read.argtypes = [cache, batch, rows, rows, C.c_void_p]
+        L.ap_kv_read.restype = C.c_int
+        L.ap_attention_workspace.argtypes = [cache, batch, C.c_uint32, C.c_uint32, C.c_uint32, C.POINTER(C.c_uint64)]
+        L.ap_attention_workspace.restype = C.c_int
+        L.ap_attention.argtypes = [cache, batch, rows, rows, C.c_uint32, C.c_float, C.c_uint32, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p]
+        L.ap_attention.restype = C.c_int
         _lib = L
     return _lib
 
@@ -317,3 +348,50 @@ def ap_agentic_destroy(handle: int) -> None:
 
 def ap_workload_destroy(workload: int) -> None:
     _check(lib().ap_workload_destroy(workload), "ap_workload_destroy")
+
+
+def make_kv_cache(dtype: int, bits: int, n_pages: int, page_size: int, kv_heads: int, head_dim: int, k_ptr: int, v_ptr: int,
+                  k_pairs_ptr: int = 0, v_pairs_ptr: int = 0, strides=None, pair_strides=None) -> ApKvCache:
+    """Describes a paged cache.  Without ``strides`` (bytes of a page, a head, a slot) it is [page][head][slot][channel], pairs
+    [page][head][slot][head_dim / 64][2]."""
+    row, pair = (2 * head_dim if bits == 16 else head_dim // 2), 4 * (head_dim // 64)
+    strides = strides or (kv_heads * page_size * row, page_size * row, row)
+    pair_strides = pair_strides or (kv_heads * page_size * pair, page_size * pair, pair)
+    return ApKvCache(dtype, bits, n_pages, page_size, kv_heads, head_dim, k_ptr, v_ptr, k_pairs_ptr or None, v_pairs_ptr or None,
+                     *strides, *(pair_strides if bits == 4 else (0, 0, 0)))
+
+
+def make_seq_batch(n_seqs: int, n_tokens: int, max_new: int, max_kv: int, new_first_ptr: int, kv_len_ptr: int, page_table_ptr: int,
+                   table_width: int, table_stride: int | None = None) -> ApSeqBatch:
+    return ApSeqBatch(n_seqs, n_tokens, max_new, max_kv, table_width, new_first_ptr, kv_len_ptr, page_table_ptr,
+                      table_width if table_stride is None else table_stride)
+
+
+def make_rows(ptr: int, heads: int, head_dim: int, token_stride: int | None = None, head_stride: int | None = None) -> ApRows:
+    """Rows [token][head][head_dim] of 2-byte values; strides in bytes where they are not contiguous."""
+    return ApRows(ptr, 2 * heads * head_dim if token_stride is None else token_stride, 2 * head_dim if head_stride is None else head_stride)
+
+
+def make_rotation(table_ptr: int, n_positions: int, rot_dim: int, neighbours: bool = False) -> ApRotation:
+    return ApRotation(table_ptr, n_positions, rot_dim, int(neighbours))
+
+
+def ap_kv_append(cache: ApKvCache, batch: ApSeqBatch, k: ApRows, v: ApRows, rotation: ApRotation | None = None, q: ApRows | None = None,
+                 q_out: ApRows | None = None, q_heads: int = 0, stream: int = 0) -> None:
+    _check(lib().ap_kv_append(cache, batch, k, v, rotation, q, q_out, q_heads, stream), "ap_kv_append")
+
+
+def ap_kv_read(cache: ApKvCache, batch: ApSeqBatch, k_out: ApRows, v_out: ApRows, stream: int = 0) -> None:
+    _check(lib().ap_kv_read(cache, batch, k_out, v_out, stream), "ap_kv_read")
+
+
+def ap_attention_workspace(cache: ApKvCache, batch: ApSeqBatch, q_heads: int, window: int = 0, sinks: int = 0) -> int:
+    """Bytes of device memory that ap_attention needs for a batch of this description."""
+    need = C.c_uint64()
+    _check(lib().ap_attention_workspace(cache, batch, q_heads, window, sinks, need), "ap_attention_workspace")
+    return need.value
+
+
+def ap_attention(cache: ApKvCache, batch: ApSeqBatch, q: ApRows, out: ApRows, q_heads: int, scale: float, window: int = 0, sinks: int = 0,
+                 workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().ap_attention(cache, batch, q, out, q_heads, scale, window, sinks, workspace_ptr, workspace_bytes, stream), "ap_attention")

@@ -6,7 +6,7 @@ import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
-SOURCES = [os.path.join(_HERE, "csrc", "ap_eval.hip")]
+SOURCES = [os.path.join(_HERE, "csrc", "ap_eval.hip"), os.path.join(_HERE, "csrc_attn", "ap_attention.hip")]
 LIB_PATH = os.path.join(_HERE, "libautopoiesis_eval.so")
 TEST_SOURCES = [os.path.join(ROOT, "tests", "device", "runs.hip")]
 TEST_LIB_PATH = os.path.join(ROOT, "tests", "device", "libruns.so")

@@ -1,0 +1,241 @@
+// C ABI of the cache and attention operators: checks of arguments, choice of kernels and grids.
+#include "at_append.hpp"
+#include "at_few.hpp"
+#include "at_many.hpp"
+
+namespace {
+
+constexpr uint64_t kMost = 1ull << 31;   // rows and positions stay below
+constexpr uint64_t kMostGroups = 1ull << 24;  // and workgroups (of 256 threads: a grid holds less than 2^32)
+
+bool multiple(const void* p, uint64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+bool stride_ok(int64_t s, int64_t n) { return s >= 0 && s % n == 0; }
+
+// magic and shift of a division of numbers below 2^31 by `d`: n / d = ((2 n) * magic >> 32) >> shift
+void divider(uint32_t d, uint32_t* magic, uint32_t* shift) {
+    uint32_t l = 0;
+    while ((1ull << l) < d) ++l;
+    *shift = l;
+    *magic = (uint32_t)(((1ull << (31 + l)) + d - 1) / d);
+}
+
+ap_status take_cache(const ap_kv_cache* c, Cache* out) {
+    if (!c || c->dtype > AP_FP16 || (c->bits != 16 && c->bits != 4) || (c->head_dim != 64 && c->head_dim != 128)) return AP_ERR_INVALID;
+    if (c->n_pages == 0 || c->page_size == 0 || c->kv_heads == 0 || !c->k || !c->v) return AP_ERR_INVALID;
+    if (!multiple(c->k, 16) || !multiple(c->v, 16)) return AP_ERR_INVALID;
+    if (!stride_ok(c->page_stride, 16) || !stride_ok(c->head_stride, 16) || !stride_ok(c->slot_stride, 16)) return AP_ERR_INVALID;
+    if (c->bits == 4) {
+        const int64_t n = 4 * (c->head_dim / 64);
+        if (!c->k_pairs || !c->v_pairs || !multiple(c->k_pairs, n) || !multiple(c->v_pairs, n)) return AP_ERR_INVALID;
+        if (!stride_ok(c->pair_page_stride, n) || !stride_ok(c->pair_head_stride, n) || !stride_ok(c->pair_slot_stride, n)) return AP_ERR_INVALID;
+    }
+    if (c->n_pages >= kMost || c->page_size >= kMost || c->kv_heads >= kMost) return AP_ERR_RANGE;
+    *out = Cache{(char*)c->k, (char*)c->v, (char*)c->k_pairs, (char*)c->v_pairs, c->page_stride, c->head_stride, c->slot_stride,
+                 c->pair_page_stride, c->pair_head_stride, c->pair_slot_stride, c->n_pages, c->page_size, 0, 0};
+    divider(c->page_size, &out->magic, &out->shift);
+    return AP_OK;
+}
+
+ap_status take_batch(const ap_kv_cache* c, const ap_seq_batch* b, Batch* out) {
+    if (!b || b->n_seqs == 0 || b->max_kv == 0 || b->table_width == 0 || !b->new_first || !b->kv_len || !b->page_table) return AP_ERR_INVALID;
+    if (b->n_tokens != 0 && b->max_new == 0) return AP_ERR_INVALID;
+    if (b->table_stride < (int64_t)b->table_width || !multiple(b->new_first, 4) || !multiple(b->kv_len, 4) || !multiple(b->page_table, 4)) return AP_ERR_INVALID;
+    if ((uint64_t)b->table_width * c->page_size < b->max_kv) return AP_ERR_RANGE;
+    if (b->max_kv >= kMost - 4096 || b->n_tokens >= kMost || b->n_seqs >= kMost) return AP_ERR_RANGE;
+    *out = Batch{b->new_first, b->kv_len, b->page_table, b->table_stride, b->n_seqs, b->n_tokens, std::min(b->max_new, b->n_tokens), b->max_kv};
+    return AP_OK;
+}
+
+ap_status take_rows(const ap_rows* r, Rows* out) {
+    if (!r || !r->data || !multiple(r->data, 16) || !stride_ok(r->token_stride, 16) || !stride_ok(r->head_stride, 16)) return AP_ERR_INVALID;
+    *out = Rows{(char*)r->data, r->token_stride, r->head_stride};
+    return AP_OK;
+}
+
+template <typename F> void for_type(uint32_t dtype, F f) { dtype == AP_BF16 ? f(bf16{}) : f(fp16{}); }
+template <typename F> void for_dim(uint32_t d, F f) { d == 128 ? f(std::integral_constant<uint32_t, 128>{}) : f(std::integral_constant<uint32_t, 64>{}); }
+template <typename F> void for_bits(uint32_t b, F f) { b == 16 ? f(std::integral_constant<uint32_t, 16>{}) : f(std::integral_constant<uint32_t, 4>{}); }
+template <typename F> void for_cache(const ap_kv_cache* c, F f) {
+    for_type(c->dtype, [&](auto e) { for_dim(c->head_dim, [&](auto d) { for_bits(c->bits, [&](auto b) { f(e, d, b); }); }); });
+}
+
+ap_status launched() { return hipGetLastError() == hipSuccess ? AP_OK : AP_ERR_DEVICE; }
+
+// Heads that a wavefront takes one after another: with few tokens a pass each, so that the call is as short as one pass;
+// with many up to four, which share the look-up of the token and its cosines.
+void row_grid(AppendParams* p, uint32_t heads, uint32_t heads_at_once, dim3* grid) {
+    uint32_t passes = 1;
+    while (passes < 4 && (uint64_t)p->batch.n_tokens * heads / (heads_at_once * passes) > 16384) passes *= 2;
+    p->heads_per_wave = heads_at_once * passes;
+    *grid = dim3((p->batch.n_tokens + kAppendThreads / kLanes - 1) / (kAppendThreads / kLanes), (heads + p->heads_per_wave - 1) / p->heads_per_wave);
+}
+
+uint32_t tiles_of(uint64_t n, uint32_t tile) { return (uint32_t)((n + tile - 1) / tile); }
+
+// Tiles of keys that `span` neighbouring new tokens can see at most.
+uint32_t most_tiles(const Batch& b, uint32_t window, uint32_t sinks, uint64_t span, uint32_t tile) {
+    if (!window) return tiles_of(b.max_kv, tile);
+    return tiles_of(std::min<uint64_t>(b.max_kv, (uint64_t)window + span - 1), tile) + tiles_of(std::min(sinks, b.max_kv), tile);
+}
+
+struct Plan {
+    bool few, many;
+    uint32_t few_tiles;                  // tiles of 16 rows
+    uint32_t few_rows, few_stride, few_chunk, few_chunks;
+    uint32_t many_chunk, many_chunks, row_tiles;
+    uint64_t few_bytes, many_bytes;
+};
+
+constexpr uint32_t kResident = 512;      // workgroups that the chip holds of either kernel: two on each of 256 CUs
+
+ap_status plan_of(const ap_kv_cache* c, const Batch& b, uint32_t q_heads, uint32_t window, uint32_t sinks, Plan* out) {
+    Plan r{};
+    const uint32_t group = q_heads / c->kv_heads;
+    const uint64_t rows = (uint64_t)b.max_new * group;
+    if ((uint64_t)b.n_tokens * q_heads >= kMost || (uint64_t)b.n_seqs * c->kv_heads >= kMost) return AP_ERR_RANGE;
+    const uint64_t row_bytes = 4 * c->head_dim + 8;
+    // A batch of one sequence, or of sequences that all have few rows, needs one kernel only; in a mixed one each takes
+    // the sequences that suit it.
+    r.few = b.n_tokens && group <= kFewRows && (rows <= kFewRows || b.n_seqs > 1);
+    r.many = b.n_tokens && rows > kFewRows;
+    if (r.few) {
+        const uint64_t most = r.many ? (group <= 16 ? 16 : kFewRows) : rows;
+        r.few_tiles = most <= 16 ? 1 : most <= 32 ? 2 : 4;
+        r.few_rows = r.many ? (uint32_t)most : kFewRows;
+        r.few_stride = (uint32_t)most;
+        const uint32_t tiles = most_tiles(b, window, sinks, std::max<uint64_t>(1, most / group), kFewKeys);
+        const uint64_t pairs = (uint64_t)b.n_seqs * c->kv_heads;
+        uint64_t chunk = (tiles * pairs + 2 * kResident - 1) / (2 * kResident);
+        chunk = std::max<uint64_t>({4, tiles / 64, std::min<uint64_t>(32, chunk)});
+        r.few_chunk = (uint32_t)((chunk + 3) / 4 * 4);
+        r.few_chunks = (tiles + r.few_chunk - 1) / r.few_chunk;
+        if (pairs * r.few_chunks >= kMostGroups) return AP_ERR_RANGE;
+        if (r.few_chunks > 1) r.few_bytes = row_bytes * r.few_chunks * pairs * r.few_stride;
+    }
+    if (r.many) {
+        r.row_tiles = (uint32_t)((uint64_t)b.n_tokens * group / kManyRows) + b.n_seqs;
+        const uint32_t tiles = most_tiles(b, window, sinks, kManyRows / group + 2, kManyKeys);
+        const uint64_t groups = ((uint64_t)b.n_tokens * group / kManyRows + 1) * c->kv_heads;
+        const uint64_t chunks = std::max<uint64_t>(1, kResident / groups);
+        r.many_chunk = (uint32_t)std::max<uint64_t>(8, (tiles + chunks - 1) / chunks);
+        r.many_chunks = (tiles + r.many_chunk - 1) / r.many_chunk;
+        if (((uint64_t)r.row_tiles) * c->kv_heads * r.many_chunks >= kMostGroups) return AP_ERR_RANGE;
+        if (r.many_chunks > 1) r.many_bytes = row_bytes * r.many_chunks * b.n_tokens * q_heads;
+    }
+    if (r.few_bytes + r.many_bytes > 0 && (uint64_t)b.n_tokens * ((q_heads + 3) / 4) >= kMostGroups) return AP_ERR_RANGE;
+    *out = r;
+    return AP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ap_status ap_kv_append(const ap_kv_cache* cache, const ap_seq_batch* batch, const ap_rows* k, const ap_rows* v, const ap_rotation* rotation,
+                       const ap_rows* q, const ap_rows* q_out, uint32_t q_heads, void* stream) {
+    AppendParams p{};
+    ap_status st = take_cache(cache, &p.cache);
+    if (st == AP_OK) st = take_batch(cache, batch, &p.batch);
+    if (st == AP_OK) st = take_rows(k, &p.k);
+    if (st == AP_OK) st = take_rows(v, &p.v);
+    if (st == AP_OK && q) {
+        if (q_heads == 0) return AP_ERR_INVALID;
+        st = take_rows(q, &p.q);
+        if (st == AP_OK) st = take_rows(q_out, &p.q_out);
+        p.q_heads = q_heads;
+    }
+    if (st != AP_OK) return st;
+    p.kv_heads = cache->kv_heads;
+    if (rotation) {
+        if (!rotation->table || !multiple(rotation->table, 16) || rotation->rot_dim == 0 || rotation->rot_dim % 16 || rotation->rot_dim > cache->head_dim)
+            return AP_ERR_INVALID;
+        if (rotation->n_positions < batch->max_kv) return AP_ERR_RANGE;
+        p.turn = rotation->table, p.rot = rotation->rot_dim;
+    }
+    const uint64_t heads = 2ull * cache->kv_heads + p.q_heads;
+    if (heads >= 65536 || batch->n_tokens >= kMostGroups || (uint64_t)batch->n_tokens * heads >= kMost) return AP_ERR_RANGE;
+    if (batch->n_tokens == 0) return AP_OK;
+    dim3 grid;
+    row_grid(&p, (uint32_t)heads, kLanes / (cache->head_dim / 16), &grid);
+    const bool halves = !(rotation && rotation->neighbours);
+    for_cache(cache, [&](auto e, auto d, auto b) {
+        auto kernel = halves ? k_append<decltype(e), d(), b(), true> : k_append<decltype(e), d(), b(), false>;
+        hipLaunchKernelGGL(kernel, grid, dim3(kAppendThreads), 0, (hipStream_t)stream, p);
+    });
+    return launched();
+}
+
+ap_status ap_kv_read(const ap_kv_cache* cache, const ap_seq_batch* batch, const ap_rows* k_out, const ap_rows* v_out, void* stream) {
+    AppendParams p{};
+    ap_status st = take_cache(cache, &p.cache);
+    if (st == AP_OK) st = take_batch(cache, batch, &p.batch);
+    if (st == AP_OK) st = take_rows(k_out, &p.k);
+    if (st == AP_OK) st = take_rows(v_out, &p.v);
+    if (st != AP_OK) return st;
+    p.kv_heads = cache->kv_heads;
+    const uint64_t heads = 2ull * cache->kv_heads;
+    if (heads >= 65536 || batch->n_tokens >= kMostGroups || (uint64_t)batch->n_tokens * heads >= kMost) return AP_ERR_RANGE;
+    if (batch->n_tokens == 0) return AP_OK;
+    dim3 grid;
+    row_grid(&p, (uint32_t)heads, kLanes / (cache->head_dim / 8), &grid);
+    for_cache(cache, [&](auto e, auto d, auto b) {
+        hipLaunchKernelGGL((k_read<decltype(e), d(), b()>), grid, dim3(kAppendThreads), 0, (hipStream_t)stream, p);
+    });
+    return launched();
+}
+
+ap_status ap_attention_workspace(const ap_kv_cache* cache, const ap_seq_batch* batch, uint32_t q_heads, uint32_t window, uint32_t sinks, uint64_t* bytes) {
+    Cache c;
+    Batch b;
+    Plan plan;
+    if (!bytes) return AP_ERR_INVALID;
+    ap_status st = take_cache(cache, &c);
+    if (st == AP_OK) st = take_batch(cache, batch, &b);
+    if (st != AP_OK) return st;
+    if (q_heads == 0 || q_heads % cache->kv_heads) return AP_ERR_INVALID;
+    st = plan_of(cache, b, q_heads, window, sinks, &plan);
+    if (st == AP_OK) *bytes = plan.few_bytes + plan.many_bytes;
+    return st;
+}
+
+ap_status ap_attention(const ap_kv_cache* cache, const ap_seq_batch* batch, const ap_rows* q, const ap_rows* out, uint32_t q_heads, float scale,
+                       uint32_t window, uint32_t sinks, void* workspace, uint64_t workspace_bytes, void* stream) {
+    AttnParams p{};
+    Plan plan;
+    ap_status st = take_cache(cache, &p.cache);
+    if (st == AP_OK) st = take_batch(cache, batch, &p.batch);
+    if (st == AP_OK) st = take_rows(q, &p.q);
+    if (st == AP_OK) st = take_rows(out, &p.out);
+    if (st != AP_OK) return st;
+    if (q_heads == 0 || q_heads % cache->kv_heads || !(scale > 0.0f) || !std::isfinite(scale)) return AP_ERR_INVALID;
+    st = plan_of(cache, p.batch, q_heads, window, sinks, &plan);
+    if (st != AP_OK) return st;
+    if (plan.few_bytes + plan.many_bytes > 0 && (!workspace || !multiple(workspace, 16) || workspace_bytes < plan.few_bytes + plan.many_bytes)) return AP_ERR_INVALID;
+    if (batch->n_tokens == 0) return AP_OK;
+    p.q_heads = q_heads, p.kv_heads = cache->kv_heads, p.group = q_heads / cache->kv_heads;
+    divider(p.group, &p.group_magic, &p.group_shift);
+    p.window = window, p.sinks = window ? sinks : 0;
+    p.scale_log2 = scale * 1.44269504088896341f;
+    p.few_rows = plan.few ? plan.few_rows : 0, p.few_stride = plan.few_stride;
+    p.few_chunk = plan.few ? plan.few_chunk : 1, p.many_chunk = plan.many ? plan.many_chunk : 1;
+    char* space = (char*)workspace;
+    const uint64_t row_bytes = 4 * cache->head_dim + 8, few_n = plan.few_bytes / row_bytes, many_n = plan.many_bytes / row_bytes;
+    p.few_o = (float*)space, p.many_o = p.few_o + few_n * cache->head_dim;
+    p.few_ml = (f32x2*)(p.many_o + many_n * cache->head_dim), p.many_ml = p.few_ml + few_n;
+    const hipStream_t on = (hipStream_t)stream;
+    for_cache(cache, [&](auto e, auto d, auto b) {
+        using E = decltype(e);
+        if (plan.few) {
+            auto kernel = plan.few_tiles == 1 ? k_attend_few<E, d(), b(), 1> : plan.few_tiles == 2 ? k_attend_few<E, d(), b(), 2> : k_attend_few<E, d(), b(), 4>;
+            hipLaunchKernelGGL(kernel, dim3(batch->n_seqs * cache->kv_heads * plan.few_chunks), dim3(kFewThreads), 0, on, p);
+        }
+        if (plan.many)
+            hipLaunchKernelGGL((k_attend_many<E, d(), b()>), dim3(plan.row_tiles * cache->kv_heads * plan.many_chunks), dim3(kManyThreads), 0, on, p,
+                               plan.row_tiles, plan.many_chunks);
+        if (plan.few_bytes + plan.many_bytes > 0)
+            hipLaunchKernelGGL((k_attend_join<E, d()>), dim3(batch->n_tokens * ((q_heads + 3) / 4)), dim3(256), 0, on, p);
+    });
+    return launched();
+}
+
+}  // extern "C"
