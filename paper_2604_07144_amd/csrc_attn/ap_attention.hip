@@ -81,36 +81,46 @@ uint32_t most_tiles(const Batch& b, uint32_t window, uint32_t sinks, uint64_t sp
 struct Plan {
     bool few, many;
     uint32_t few_tiles;                  // tiles of 16 rows
-    uint32_t few_rows, few_stride, few_chunk, few_chunks;
+    uint32_t few_rows, few_stride, few_groups, few_seqs;
     uint32_t many_chunk, many_chunks, row_tiles;
-    uint64_t few_bytes, many_bytes;
+    uint64_t few_n, many_n;              // rows of results in the workspace
+    uint64_t plan_bytes, bytes;
 };
 
 constexpr uint32_t kResident = 512;      // workgroups that the chip holds of either kernel: two on each of 256 CUs
+
+// Short sequences are not split (a wavefront takes a whole sequence and head, and nothing is left to join): the join costs
+// about 4 us, a tile of a wavefront on its own about 1.1 us.  32 heads on 8, 128 channels, bf16, us whole / split and joined:
+// 8 sequences of 64 keys 7.1 / 10.9, of 128 9.3 / 11.0, of 192 11.5 / 11.4, of 256 13.8 / 11.9; with 64 sequences, whose 512
+// pieces fill half the chip, of 256 16.8 / 20.9 (4 bits 16.2 / 17.9), of 512 34.5 / 36.6 (4 bits 25.7 / 20.9).
+constexpr uint32_t kUnsplitTiles = 5, kUnsplitTilesOfMany = 8, kManyPairs = 512;
+constexpr uint32_t kFewLeast = 2;        // places of the line that a wavefront of the kernel of few rows takes at least
 
 ap_status plan_of(const ap_kv_cache* c, const Batch& b, uint32_t q_heads, uint32_t window, uint32_t sinks, Plan* out) {
     Plan r{};
     const uint32_t group = q_heads / c->kv_heads;
     const uint64_t rows = (uint64_t)b.max_new * group;
     if ((uint64_t)b.n_tokens * q_heads >= kMost || (uint64_t)b.n_seqs * c->kv_heads >= kMost) return AP_ERR_RANGE;
-    const uint64_t row_bytes = 4 * c->head_dim + 8;
     // A batch of one sequence, or of sequences that all have few rows, needs one kernel only; in a mixed one each takes
     // the sequences that suit it.
     r.few = b.n_tokens && group <= kFewRows && (rows <= kFewRows || b.n_seqs > 1);
     r.many = b.n_tokens && rows > kFewRows;
     if (r.few) {
         const uint64_t most = r.many ? (group <= 16 ? 16 : kFewRows) : rows;
-        r.few_tiles = most <= 16 ? 1 : most <= 32 ? 2 : 4;
+        r.few_tiles = most <= 16 ? 1 : 2;
         r.few_rows = r.many ? (uint32_t)most : kFewRows;
         r.few_stride = (uint32_t)most;
         const uint32_t tiles = most_tiles(b, window, sinks, std::max<uint64_t>(1, most / group), kFewKeys);
-        const uint64_t pairs = (uint64_t)b.n_seqs * c->kv_heads;
-        uint64_t chunk = (tiles * pairs + 2 * kResident - 1) / (2 * kResident);
-        chunk = std::max<uint64_t>({4, tiles / 64, std::min<uint64_t>(32, chunk)});
-        r.few_chunk = (uint32_t)((chunk + 3) / 4 * 4);
-        r.few_chunks = (tiles + r.few_chunk - 1) / r.few_chunk;
-        if (pairs * r.few_chunks >= kMostGroups) return AP_ERR_RANGE;
-        if (r.few_chunks > 1) r.few_bytes = row_bytes * r.few_chunks * pairs * r.few_stride;
+        r.few_seqs = std::min(b.n_seqs, kFewSeqs);
+        const uint64_t pairs = (uint64_t)r.few_seqs * c->kv_heads, units = pairs * ((uint64_t)tiles + kFewEnter);
+        if (units >= kMost || pairs * r.few_stride >= kMostGroups) return AP_ERR_RANGE;
+        if (tiles <= (pairs >= kManyPairs ? kUnsplitTilesOfMany : kUnsplitTiles)) {
+            r.few_groups = (uint32_t)((pairs + kFewWaves - 1) / kFewWaves);
+        } else {
+            r.few_groups = (uint32_t)std::min<uint64_t>((units + kFewWaves - 1) / kFewWaves, kResident);
+            r.plan_bytes = (4ull * (r.few_seqs + 2) + 15) / 16 * 16;
+            r.few_n = 2ull * r.few_groups * kFewWaves * r.few_stride;
+        }
     }
     if (r.many) {
         r.row_tiles = (uint32_t)((uint64_t)b.n_tokens * group / kManyRows) + b.n_seqs;
@@ -120,9 +130,12 @@ ap_status plan_of(const ap_kv_cache* c, const Batch& b, uint32_t q_heads, uint32
         r.many_chunk = (uint32_t)std::max<uint64_t>(8, (tiles + chunks - 1) / chunks);
         r.many_chunks = (tiles + r.many_chunk - 1) / r.many_chunk;
         if (((uint64_t)r.row_tiles) * c->kv_heads * r.many_chunks >= kMostGroups) return AP_ERR_RANGE;
-        if (r.many_chunks > 1) r.many_bytes = row_bytes * r.many_chunks * b.n_tokens * q_heads;
+        if (r.many_chunks > 1) {
+            r.many_n = (uint64_t)r.many_chunks * b.n_tokens * q_heads;
+            if ((uint64_t)b.n_tokens * ((q_heads + 3) / 4) >= kMostGroups) return AP_ERR_RANGE;
+        }
     }
-    if (r.few_bytes + r.many_bytes > 0 && (uint64_t)b.n_tokens * ((q_heads + 3) / 4) >= kMostGroups) return AP_ERR_RANGE;
+    r.bytes = r.plan_bytes + (4ull * c->head_dim + 8) * (r.few_n + r.many_n);
     *out = r;
     return AP_OK;
 }
@@ -194,7 +207,7 @@ ap_status ap_attention_workspace(const ap_kv_cache* cache, const ap_seq_batch* b
     if (st != AP_OK) return st;
     if (q_heads == 0 || q_heads % cache->kv_heads) return AP_ERR_INVALID;
     st = plan_of(cache, b, q_heads, window, sinks, &plan);
-    if (st == AP_OK) *bytes = plan.few_bytes + plan.many_bytes;
+    if (st == AP_OK) *bytes = plan.bytes;
     return st;
 }
 
@@ -210,30 +223,37 @@ ap_status ap_attention(const ap_kv_cache* cache, const ap_seq_batch* batch, cons
     if (q_heads == 0 || q_heads % cache->kv_heads || !(scale > 0.0f) || !std::isfinite(scale)) return AP_ERR_INVALID;
     st = plan_of(cache, p.batch, q_heads, window, sinks, &plan);
     if (st != AP_OK) return st;
-    if (plan.few_bytes + plan.many_bytes > 0 && (!workspace || !multiple(workspace, 16) || workspace_bytes < plan.few_bytes + plan.many_bytes)) return AP_ERR_INVALID;
+    if (plan.bytes > 0 && (!workspace || !multiple(workspace, 16) || workspace_bytes < plan.bytes)) return AP_ERR_INVALID;
     if (batch->n_tokens == 0) return AP_OK;
     p.q_heads = q_heads, p.kv_heads = cache->kv_heads, p.group = q_heads / cache->kv_heads;
     divider(p.group, &p.group_magic, &p.group_shift);
     p.window = window, p.sinks = window ? sinks : 0;
     p.scale_log2 = scale * 1.44269504088896341f;
     p.few_rows = plan.few ? plan.few_rows : 0, p.few_stride = plan.few_stride;
-    p.few_chunk = plan.few ? plan.few_chunk : 1, p.many_chunk = plan.many ? plan.many_chunk : 1;
+    p.few_waves = plan.few_groups * kFewWaves, p.few_least = kFewLeast, p.many_chunk = plan.many_chunk;
     char* space = (char*)workspace;
-    const uint64_t row_bytes = 4 * cache->head_dim + 8, few_n = plan.few_bytes / row_bytes, many_n = plan.many_bytes / row_bytes;
-    p.few_o = (float*)space, p.many_o = p.few_o + few_n * cache->head_dim;
-    p.few_ml = (f32x2*)(p.many_o + many_n * cache->head_dim), p.many_ml = p.few_ml + few_n;
+    p.few_plan = plan.plan_bytes ? (uint32_t*)space : nullptr;
+    p.few_o = (float*)(space + plan.plan_bytes), p.many_o = p.few_o + plan.few_n * cache->head_dim;
+    p.few_ml = (f32x2*)(p.many_o + plan.many_n * cache->head_dim), p.many_ml = p.few_ml + plan.few_n;
     const hipStream_t on = (hipStream_t)stream;
     for_cache(cache, [&](auto e, auto d, auto b) {
         using E = decltype(e);
         if (plan.few) {
-            auto kernel = plan.few_tiles == 1 ? k_attend_few<E, d(), b(), 1> : plan.few_tiles == 2 ? k_attend_few<E, d(), b(), 2> : k_attend_few<E, d(), b(), 4>;
-            hipLaunchKernelGGL(kernel, dim3(batch->n_seqs * cache->kv_heads * plan.few_chunks), dim3(kFewThreads), 0, on, p);
+            auto kernel = plan.few_tiles == 1 ? k_attend_few<E, d(), b(), 1> : k_attend_few<E, d(), b(), 2>;
+            for (uint32_t s = 0; s < batch->n_seqs; s += kFewSeqs) {    // so many sequences a launch, one launch after the other in one workspace
+                AttnParams x = p;
+                x.batch.n_seqs = std::min(kFewSeqs, batch->n_seqs - s);
+                x.batch.first += s, x.batch.kv_len += s, x.batch.table += (int64_t)s * p.batch.table_stride;
+                const uint32_t pairs = x.batch.n_seqs * p.kv_heads;
+                hipLaunchKernelGGL(kernel, dim3(plan.few_groups), dim3(kFewThreads), 0, on, x);
+                if (p.few_plan) hipLaunchKernelGGL((k_join_few<E, d()>), dim3((pairs * plan.few_stride + 3) / 4), dim3(256), 0, on, x);
+            }
         }
-        if (plan.many)
+        if (plan.many) {
             hipLaunchKernelGGL((k_attend_many<E, d(), b()>), dim3(plan.row_tiles * cache->kv_heads * plan.many_chunks), dim3(kManyThreads), 0, on, p,
                                plan.row_tiles, plan.many_chunks);
-        if (plan.few_bytes + plan.many_bytes > 0)
-            hipLaunchKernelGGL((k_attend_join<E, d()>), dim3(batch->n_tokens * ((q_heads + 3) / 4)), dim3(256), 0, on, p);
+            if (plan.many_chunks > 1) hipLaunchKernelGGL((k_join_many<E, d()>), dim3(batch->n_tokens * ((q_heads + 3) / 4)), dim3(256), 0, on, p);
+        }
     });
     return launched();
 }

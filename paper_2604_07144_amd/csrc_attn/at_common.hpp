@@ -100,6 +100,12 @@ __device__ __forceinline__ Seq seq_at(const Batch& b, uint32_t s) {
     return r;
 }
 
+// The same number, but computed here: keeps what depends on it from being moved out of a loop and held in registers.
+__device__ __forceinline__ uint32_t here(uint32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 template <typename E> __device__ __forceinline__ uint16_t bits16(E x) { return __builtin_bit_cast(uint16_t, x); }
 template <typename E> __device__ __forceinline__ E from_bits16(uint32_t x) { return __builtin_bit_cast(E, (uint16_t)x); }
 

@@ -280,6 +280,26 @@ __global__ __launch_bounds__(kManyThreads, 2) void k_attend_many(const AttnParam
     }
 }
 
+// Joins the chunks of a row: a wavefront takes one row (token, head).
+template <typename E, uint32_t D>
+__global__ __launch_bounds__(256) void k_join_many(const AttnParams p) {
+    const uint32_t per_token = (p.q_heads + 3) / 4;
+    const uint32_t t = blockIdx.x / per_token, h = blockIdx.x % per_token * 4 + threadIdx.x / kLanes;
+    if (h >= p.q_heads) return;
+    const uint32_t s = seq_of(p.batch, t);
+    if (s >= p.batch.n_seqs) return;
+    const Seq seq = seq_at(p.batch, s);
+    const int32_t n_new = min(seq.n_new, (int32_t)p.batch.max_new), i = (int32_t)t - seq.first;
+    const uint32_t rows = (uint32_t)n_new * p.group;
+    if (i < 0 || i >= n_new || rows <= p.few_rows) return;
+    const uint32_t head = h / p.group, row = (uint32_t)i * p.group + h - head * p.group;
+    const uint32_t r0 = row / kManyRows * kManyRows, r1 = min(r0 + kManyRows, rows) - 1;
+    const uint32_t n = (span_of<kManyKeys>(p, seq, (int32_t)over_group(p, r0), (int32_t)over_group(p, r1)).tiles + p.many_chunk - 1) / p.many_chunk;
+    if (n <= 1) return;                                     // written already
+    join_row<E, D>(p.many_o, p.many_ml, [&](uint32_t z) { return ((uint64_t)z * p.batch.n_tokens + t) * p.q_heads + h; }, n,
+                   p.out.data + (int64_t)t * p.out.token_stride + (int64_t)h * p.out.head_stride);
+}
+
 }  // namespace
 
 #endif  // AT_MANY_HPP

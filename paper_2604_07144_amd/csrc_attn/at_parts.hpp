@@ -20,10 +20,14 @@ struct AttnParams {
     uint32_t window, sinks;              // window 0: none
     float scale_log2;                    // scale * log2(e)
     uint32_t few_rows;                   // sequences with at most so many rows go to the kernel of few rows, the others to that of many
-    uint32_t few_chunk, many_chunk;      // tiles of keys that a workgroup of either takes
+    uint32_t few_waves, few_least;       // few rows: so many wavefronts share the line of tiles, at least so many tiles each
     uint32_t few_stride;                 // rows that a (sequence, kv head) has in the workspace
-    float *few_o, *many_o;               // what the chunks of a row found: [chunk][sequence][kv head][row][D], [chunk][new token][query head][D]
-    f32x2 *few_ml, *many_ml;             // and its (m, l)
+    uint32_t* few_plan;                  // null: a wavefront takes a whole (sequence, kv head); otherwise workspace: tiles of a wavefront, then the line (tiles of the sequences before each)
+    float* few_o;                        // [wavefront][2][row][D]: what the pieces that do not cover their sequence found
+    f32x2* few_ml;                       // and its (m, l)
+    uint32_t many_chunk;                 // many rows: tiles of keys that a workgroup takes
+    float* many_o;                       // [chunk][new token][query head][D]
+    f32x2* many_ml;
 };
 
 __device__ __forceinline__ uint32_t over_group(const AttnParams& p, uint32_t row) {
@@ -73,56 +77,57 @@ template <typename E> constexpr uint32_t kExponent = std::is_same_v<E, bf16> ? 0
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126: 0
 
-// Joins the chunks of a row: a wavefront takes one row (token, head), a lane D / 64 of its channels.
-template <typename E, uint32_t D>
-__global__ __launch_bounds__(256) void k_attend_join(const AttnParams p) {
-    const uint32_t lane = threadIdx.x & (kLanes - 1);
-    const uint32_t per_token = (p.q_heads + 3) / 4;
-    const uint32_t t = blockIdx.x / per_token, h = blockIdx.x % per_token * 4 + threadIdx.x / kLanes;
-    if (h >= p.q_heads) return;
-    const uint32_t s = seq_of(p.batch, t);
-    if (s >= p.batch.n_seqs) return;
-    const Seq seq = seq_at(p.batch, s);
-    const int32_t n_new = min(seq.n_new, (int32_t)p.batch.max_new), i = (int32_t)t - seq.first;
-    const uint32_t rows = (uint32_t)n_new * p.group;
-    if (i < 0 || i >= n_new) return;
-    const uint32_t head = h / p.group, row = (uint32_t)i * p.group + h - head * p.group;
-    uint32_t n;
-    const float* part_o;
-    const f32x2* part_ml;
-    uint64_t at, stride;
-    if (rows <= p.few_rows) {
-        part_o = p.few_o, part_ml = p.few_ml;
-        at = ((uint64_t)s * p.kv_heads + head) * p.few_stride + row, stride = (uint64_t)p.batch.n_seqs * p.kv_heads * p.few_stride;
-        n = (span_of<kFewKeys>(p, seq, 0, n_new - 1).tiles + p.few_chunk - 1) / p.few_chunk;
-    } else {
-        part_o = p.many_o, part_ml = p.many_ml;
-        at = (uint64_t)t * p.q_heads + h, stride = (uint64_t)p.batch.n_tokens * p.q_heads;
-        const uint32_t r0 = row / kManyRows * kManyRows, r1 = min(r0 + kManyRows, rows) - 1;
-        n = (span_of<kManyKeys>(p, seq, (int32_t)(r0 / p.group), (int32_t)(r1 / p.group)).tiles + p.many_chunk - 1) / p.many_chunk;
+// Joins the parts of a row, which lie at `at(0)` .. `at(n - 1)`.  Each lane has the (m, l) of a part; then 16 lanes read the
+// channels of a part, four parts at a time and four such rounds in flight, so that a row costs three trips to memory
+// however many parts it has (up to 16).
+template <typename E, uint32_t D, typename F>
+__device__ __forceinline__ void join_row(const float* __restrict__ o, const f32x2* __restrict__ ml, F at, uint32_t n, char* dst) {
+    constexpr uint32_t kPer = D / 16;                       // channels of a lane
+    const uint32_t lane = threadIdx.x & (kLanes - 1), set = lane / 16, c0 = lane % 16 * kPer;
+    float top = -INFINITY, total = 0.0f, acc[kPer];
+#pragma unroll
+    for (uint32_t c = 0; c < kPer; ++c) acc[c] = 0.0f;
+    for (uint32_t z0 = 0; z0 < n; z0 += kLanes) {
+        const uint32_t here_n = min(n - z0, kLanes);
+        const f32x2 mine = lane < here_n ? ml[at(z0 + lane)] : f32x2{-INFINITY, 0.0f};
+        float grown = mine[0];
+#pragma unroll
+        for (uint32_t m = 1; m < kLanes; m *= 2) grown = fmaxf(grown, __shfl_xor(grown, m));
+        grown = fmaxf(grown, top);
+        const float from = grown == -INFINITY ? 0.0f : grown, keep = exp2_of(top - from), weight = exp2_of(mine[0] - from);
+        top = grown;
+        total = total * keep + weight * mine[1];            // each lane has its parts' share
+#pragma unroll
+        for (uint32_t c = 0; c < kPer; ++c) acc[c] *= keep;
+        for (uint32_t z = 0; z < here_n; z += 16) {
+            f32x4 x[4][kPer / 4];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const f32x4* src = reinterpret_cast<const f32x4*>(o + at(z0 + min(z + 4 * i + set, here_n - 1)) * D + c0);
+#pragma unroll
+                for (uint32_t c = 0; c < kPer / 4; ++c) x[i][c] = src[c];
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const float f = __shfl(weight, z + 4 * i + set);     // 0 beyond the last part
+#pragma unroll
+                for (uint32_t c = 0; c < kPer; ++c) acc[c] += f == 0.0f ? 0.0f : f * x[i][c / 4][c % 4];
+            }
+        }
     }
-    if (n <= 1) return;                                     // written already
-    float top = -INFINITY;
-    for (uint32_t z = lane; z < n; z += kLanes) top = fmaxf(top, part_ml[at + z * stride][0]);
 #pragma unroll
-    for (uint32_t m = 1; m < kLanes; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-    const float from = top == -INFINITY ? 0.0f : top;
-    float total = 0.0f, acc[D / 64];
+    for (uint32_t m = 1; m < kLanes; m *= 2) total += __shfl_xor(total, m);
 #pragma unroll
-    for (uint32_t c = 0; c < D / 64; ++c) acc[c] = 0.0f;
-#pragma unroll 4
-    for (uint32_t z = 0; z < n; ++z) {
-        const f32x2 ml = part_ml[at + z * stride];
-        const float f = exp2_of(ml[0] - from);
-        const float* src = part_o + (at + z * stride) * D + lane * (D / 64);
-        total += f * ml[1];
-#pragma unroll
-        for (uint32_t c = 0; c < D / 64; ++c) acc[c] += ml[0] == -INFINITY ? 0.0f : f * src[c];
+    for (uint32_t c = 0; c < kPer; ++c) {
+        acc[c] += __shfl_xor(acc[c], 16);
+        acc[c] += __shfl_xor(acc[c], 32);
     }
     const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-    char* dst = p.out.data + (int64_t)t * p.out.token_stride + (int64_t)h * p.out.head_stride;
-    if constexpr (D == 128) reinterpret_cast<uint32_t*>(dst)[lane] = pack2<E>(acc[0] * inv, acc[1] * inv);
-    else reinterpret_cast<E*>(dst)[lane] = (E)(acc[0] * inv);
+    if (set == 0) {
+        uint32_t* to = reinterpret_cast<uint32_t*>(dst + 2 * c0);
+#pragma unroll
+        for (uint32_t c = 0; c < kPer; c += 2) to[c / 2] = pack2<E>(acc[c] * inv, acc[c + 1] * inv);
+    }
 }
 
 }  // namespace
