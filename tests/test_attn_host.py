@@ -153,4 +153,5 @@ def test_workspaces_do_not_grow_with_the_length():
     long = b.ap_attention_workspace(_cache(), batch(1 << 20, 1), 8)
     assert 0 < long == b.ap_attention_workspace(_cache(), batch(1 << 22, 1), 8)      # pieces are as many as wavefronts
     assert b.ap_attention_workspace(_cache(), batch(1 << 20, 1), 8, 100, 4) == 0     # a window makes them short
-    assert b.ap_attention_workspace(_cache(), batch(1 << 20, 4096), 8) == 0          # many rows: enough work without a split
+    whole = b.make_seq_batch(1, 16384, 16384, 1 << 20, AT, AT, AT, 1 << 16)
+    assert b.ap_attention_workspace(_cache(), whole, 8) == 0                         # many rows: enough work without a split
