@@ -106,6 +106,10 @@ __device__ __forceinline__ uint32_t here(uint32_t x) {
     return x;
 }
 
+// A number that is the same in all lanes, in a scalar register.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
 template <typename E> __device__ __forceinline__ uint16_t bits16(E x) { return __builtin_bit_cast(uint16_t, x); }
 template <typename E> __device__ __forceinline__ E from_bits16(uint32_t x) { return __builtin_bit_cast(E, (uint16_t)x); }
 

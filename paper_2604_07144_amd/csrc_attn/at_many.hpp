@@ -1,14 +1,15 @@
-// Attention of many rows: whole prompts and chunks of them.  A workgroup takes 128 rows of one sequence and key/value
+// Attention of many rows: whole prompts and chunks of them.  A workgroup takes some rows of one sequence and key/value
 // head (a row is a new token and one of the query heads that share the key/value head, so keys and values are read once
 // for all of them) and goes over the keys that they see, 64 at a time.
 //
-// Mathematics as in the kernel of few rows.  Matrix products bound this: 4 * D operations per row and key, against
-// 4 * D bytes per key that serve 128 rows.  S^T = K Q^T and O^T = V^T P^T on 32x32x16 tiles: a wavefront has 32 rows as
-// columns, its queries and results stay in registers, the weights go from the first product's result registers to the
-// second's operands without moving, and the maximum of a row is over one lane's registers and one exchange between the
-// halves of the wavefront.  The maximum that weights are taken against is only raised when a score passes it by 2^8,
-// which 32-bit sums and 16-bit weights both have room for.  Keys and values of the next 64 positions are on their way
-// to registers while the present ones, in one of two LDS buffers, are worked on.
+// Mathematics as in the kernel of few rows.  The matrix units and the exponentials bound this together: 64 keys cost a
+// wavefront's 32 rows about 1000 cycles of either (128 channels).  S^T = K Q^T and O^T = V^T P^T on 32x32x16 tiles: a
+// wavefront has 32 rows as columns, its queries and results stay in registers, the weights go from the first product's
+// result registers to the second's operands without moving, and the maximum of a row is over one lane's registers and one
+// exchange between the halves of the wavefront.  The maximum that weights are taken against is only raised when a score
+// passes it by 2^8, which 32-bit sums and 16-bit weights both have room for.  Two wavefronts of a SIMD take turns at the
+// matrix units and the exponentials.  The next 64 keys and values are on their way to the other of two LDS buffers while
+// the present ones are worked on: in 16 bits without passing through registers, in 4 bits decoded on the way.
 #ifndef AT_MANY_HPP
 #define AT_MANY_HPP
 
@@ -16,15 +17,16 @@
 
 namespace {
 
-constexpr uint32_t kManyWaves = 4, kManyThreads = kManyWaves * kLanes;
 constexpr float kHeadroom = 8.0f;
+
+__device__ const u32x4 kZeroRow[16] = {};                   // stands in for keys and values that are not there
 
 template <typename E> __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
     if constexpr (std::is_same_v<E, bf16>) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Vec8<bf16>, a), __builtin_bit_cast(Vec8<bf16>, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(Vec8<fp16>, a), __builtin_bit_cast(Vec8<fp16>, b), c, 0, 0, 0);
 }
 
-// max over the two halves of the wavefront
+// max and sum over the two halves of the wavefront
 __device__ __forceinline__ float max_halves(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -34,30 +36,42 @@ __device__ __forceinline__ float sum_halves(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Where 16-byte piece `c` of a key's (value's) row lies in LDS.  Keys: the 16 rows that a read takes at once hold the
-// same piece in 16 different places.  Values: the 64 bytes of 4 rows that a transposing read takes at once likewise.
-template <uint32_t D> __device__ __forceinline__ uint32_t key_piece(uint32_t key, uint32_t c) {
-    return key * (D / 8) + (D == 128 ? c ^ (key & 15u) : c ^ ((key >> 1) & 7u));
+// 16 bytes of each lane from memory to LDS, to `to` + 16 * lane.  The data passes no register, so that nothing here is in
+// flight that the compiler could take for there; wait_loads() has to come between it and the barrier after which it is read.
+// (m0, which the compiler keeps nothing in across statements, says where in LDS.)
+__device__ __forceinline__ void load_to_lds(const char* from, const void* to) {
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(at), "v"(from) : "memory");
 }
-template <uint32_t D> __device__ __forceinline__ uint32_t value_piece(uint32_t key, uint32_t c) {
-    return key * (D / 8) + (D == 128 ? c ^ ((key & 3u) << 2) : c ^ (((key >> 1) & 1u) << 2));
+__device__ __forceinline__ void wait_loads() {
+    __builtin_amdgcn_s_waitcnt(0x0F70);                     // vmcnt(0); the compiler knows of it, and waits for none of its own loads again
+    asm volatile("" : : : "memory");
 }
+
+// Where 16-byte piece `c` of a key's (value's) row lies in LDS, in its row.  Keys: the 16 rows that a read takes at once
+// hold the same piece in 16 different places.  Values: the 64 bytes of 4 rows that a transposing read takes at once likewise.
+template <uint32_t D> __device__ __forceinline__ uint32_t key_piece(uint32_t key, uint32_t c) { return D == 128 ? c ^ (key & 15u) : c ^ ((key >> 1) & 7u); }
+template <uint32_t D> __device__ __forceinline__ uint32_t value_piece(uint32_t key, uint32_t c) { return D == 128 ? c ^ ((key & 3u) << 2) : c ^ (((key >> 1) & 1u) << 2); }
 
 // Workgroups: [tile of rows, last first][chunk][kv head]: late rows see most keys, and the heads of a tile, whose keys
 // are other memory, spread over the XCDs while all tiles of a head stay on one.
 template <typename E, uint32_t D, uint32_t kBits>
-__global__ __launch_bounds__(kManyThreads, 2) void k_attend_many(const AttnParams p, const uint32_t n_row_tiles, const uint32_t n_chunks) {
-    constexpr uint32_t kSteps = D / 16, kOut = D / 32, kPieces = D / 8, kRowsAtOnce = kManyThreads / kPieces, kLoads = kManyKeys / kRowsAtOnce;
+__global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) void k_attend_many(const AttnParams p, const uint32_t n_row_tiles, const uint32_t n_chunks) {
+    constexpr uint32_t kSteps = D / 16, kOut = D / 32, kPieces = D / 8;
     __shared__ u32x4 lds_k[2][kManyKeys * kPieces], lds_v[2][kManyKeys * kPieces];
-    __shared__ uint32_t lds_seen[2][kManyKeys];
+    __shared__ const char *lds_at_k[2][kManyKeys], *lds_at_v[2][kManyKeys];                // where the rows of a tile lie
+    __shared__ int64_t lds_pairs[kBits == 4 ? 2 : 1][kManyKeys];
+    __shared__ uint32_t lds_strange;                        // the last tile, counted from 1, whose values hold a NaN or an infinity
+    __shared__ uint64_t lds_seen[4];                        // one bit a key: it is there; written two tiles ahead, while the present one's is read
 
     const uint32_t head = blockIdx.x % p.kv_heads, tz = blockIdx.x / p.kv_heads, z = tz % n_chunks, slot = n_row_tiles - 1 - tz / n_chunks;
     const uint32_t lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes), col = lane % 32, half = lane / 32;
 
-    // Sequence s has the row tiles from first[s] * group / 128 + s on up to the next one's, which is never too few.
+    // Sequence s has the row tiles from first[s] * group / kManyRows + s on up to the next one's, which is never too few.
     auto begins = [&](uint32_t i) { return (uint32_t)((uint64_t)(uint32_t)p.batch.first[i] * p.group / kManyRows) + i; };
-    const uint32_t s = count_to(p.batch.n_seqs - 1, slot, begins), slot0 = begins(s);
-    const Seq seq = seq_at(p.batch, s);
+    const uint32_t s = uniform(count_to(p.batch.n_seqs - 1, slot, begins)), slot0 = uniform(begins(s));
+    Seq seq = seq_at(p.batch, s);
+    seq = Seq{uniform(seq.first), uniform(seq.n_new), uniform(seq.kv_len), uniform(seq.pos0)};
     const int32_t n_new = min(seq.n_new, (int32_t)p.batch.max_new);
     const uint32_t rows = (uint32_t)n_new * p.group;
     if (slot < slot0 || (uint64_t)(slot - slot0) * kManyRows >= rows || rows <= p.few_rows) return;
@@ -69,14 +83,14 @@ __global__ __launch_bounds__(kManyThreads, 2) void k_attend_many(const AttnParam
 
     const uint32_t r = min(row0 + wave * 32 + col, rows - 1), token = over_group(p, r);
     const int32_t pos = seq.pos0 + (int32_t)token;
-    const uint32_t q_head = head * p.group + r - token * p.group;
+    const int32_t behind = p.window ? (int32_t)max((int64_t)pos - p.window, (int64_t)INT32_MIN) : INT32_MIN;   // a key is seen from behind + 1 on
     // positions of the wavefront's first and last row
     const int32_t pos_first = seq.pos0 + (int32_t)over_group(p, min(row0 + wave * 32, rows - 1));
     const int32_t pos_last = seq.pos0 + (int32_t)over_group(p, min(row0 + wave * 32 + 31, rows - 1));
 
     u32x4 q[kSteps];
     {
-        const char* row = p.q.data + (int64_t)(seq.first + (int32_t)token) * p.q.token_stride + (int64_t)q_head * p.q.head_stride;
+        const char* row = p.q.data + (int64_t)(seq.first + (int32_t)token) * p.q.token_stride + (int64_t)(head * p.group + r - token * p.group) * p.q.head_stride;
 #pragma unroll
         for (uint32_t i = 0; i < kSteps; ++i) q[i] = *reinterpret_cast<const u32x4*>(row + 32 * i + 16 * half);
     }
@@ -89,104 +103,178 @@ __global__ __launch_bounds__(kManyThreads, 2) void k_attend_many(const AttnParam
 
     const int32_t* table = p.batch.table + (int64_t)s * p.batch.table_stride;
     const int64_t head_at = (int64_t)head * p.cache.head_stride, pair_head_at = (int64_t)head * p.cache.pair_head_stride;
-    const uint32_t my_piece = threadIdx.x % kPieces, my_key = threadIdx.x / kPieces;
-    u32x4 next_k[kLoads], next_v[kLoads];
-    uint32_t pair_k[kLoads], pair_v[kLoads];
-    bool next_there[kLoads];
-    Place ahead[kLoads];
 
+    // ---- where a tile's keys lie: one wavefront looks them up, a lane a key, two tiles ahead
+    Place ahead;
     auto places = [&](uint32_t tile) {
         int32_t base, end;
         tile_at<kManyKeys>(sp, tile, base, end);
-        const bool in = tile < last_tile;
-#pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i)
-            ahead[i] = place_of(p.cache, table, in ? (uint32_t)(base + (int32_t)(my_key + i * kRowsAtOnce)) : 0xFFFFFFFFu, (uint32_t)end);
+        ahead = place_of(p.cache, table, tile < last_tile ? (uint32_t)(base + (int32_t)lane) : 0xFFFFFFFFu, (uint32_t)end);
     };
-    auto fetch = [&]() {
+    auto put_places = [&](uint32_t tile) {                  // counted from the first
+        const uint32_t buf = tile & 1u;
+        const uint64_t seen = __ballot(ahead.there);
+        const int64_t row = ahead.page * p.cache.page_stride + ahead.slot * p.cache.slot_stride + head_at;
+        const char* zero = kBits == 16 ? reinterpret_cast<const char*>(kZeroRow) : nullptr;
+        lds_at_k[buf][lane] = ahead.there ? p.cache.k + row : zero;
+        lds_at_v[buf][lane] = ahead.there ? p.cache.v + row : zero;
+        if constexpr (kBits == 4) lds_pairs[buf][lane] = ahead.page * p.cache.pair_page_stride + ahead.slot * p.cache.pair_slot_stride + pair_head_at;
+        if (lane == 0) lds_seen[tile & 3u] = seen;
+    };
+
+    // ---- how a tile comes to LDS.  16 bits: an instruction takes kRows whole rows; lanes ask for the pieces in the order in
+    // which they shall lie.  4 bits: a thread takes 16 bytes of codes, 32 channels, of a key and a value.
+    constexpr uint32_t kRows = kLanes / kPieces, kLoads = kManyKeys / kRows / kManyWaves;
+    constexpr uint32_t kCodePieces = D / 32, kCodeThreads = kManyKeys * kCodePieces;
+    u32x4 raw_k = {0, 0, 0, 0}, raw_v = {0, 0, 0, 0};
+    uint32_t pair_k = 0, pair_v = 0;
+    const uint32_t code_key = threadIdx.x / kCodePieces, code_piece = threadIdx.x % kCodePieces;
+    auto fetch = [&](uint32_t buf) {
+        if constexpr (kBits == 16) {
 #pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i) {
-            next_there[i] = ahead[i].there;
-            const int64_t page = ahead[i].there ? ahead[i].page : 0, at = ahead[i].there ? ahead[i].slot : 0;
-            const int64_t row = page * p.cache.page_stride + at * p.cache.slot_stride + head_at;
-            if constexpr (kBits == 16) {
-                next_k[i] = *reinterpret_cast<const u32x4*>(p.cache.k + row + 16 * my_piece);
-                next_v[i] = *reinterpret_cast<const u32x4*>(p.cache.v + row + 16 * my_piece);
-            } else {
-                const int64_t pr = page * p.cache.pair_page_stride + at * p.cache.pair_slot_stride + pair_head_at + 4 * (my_piece / 8);
-                next_k[i][0] = *reinterpret_cast<const uint32_t*>(p.cache.k + row + 4 * my_piece);
-                next_v[i][0] = *reinterpret_cast<const uint32_t*>(p.cache.v + row + 4 * my_piece);
-                pair_k[i] = *reinterpret_cast<const uint32_t*>(p.cache.k_pairs + pr);
-                pair_v[i] = *reinterpret_cast<const uint32_t*>(p.cache.v_pairs + pr);
+            for (uint32_t i = 0; i < kLoads; ++i) {
+                const uint32_t at = (i * kManyWaves + wave) * kRows, key = at + lane / kPieces, c = lane % kPieces;
+                load_to_lds(lds_at_k[buf][key] + 16 * key_piece<D>(key, c), &lds_k[buf][at * kPieces]);
+                load_to_lds(lds_at_v[buf][key] + 16 * value_piece<D>(key, c), &lds_v[buf][at * kPieces]);
+            }
+        } else if (kCodeThreads >= kManyThreads || threadIdx.x < kCodeThreads) {
+            const char *at_k = lds_at_k[buf][code_key], *at_v = lds_at_v[buf][code_key];
+            const int64_t pr = lds_pairs[buf][code_key] + 4 * (code_piece / 2);
+            raw_k = raw_v = u32x4{0, 0, 0, 0}, pair_k = pair_v = 0;
+            if (at_k) {
+                raw_k = *reinterpret_cast<const u32x4*>(at_k + 16 * code_piece);
+                raw_v = *reinterpret_cast<const u32x4*>(at_v + 16 * code_piece);
+                pair_k = *reinterpret_cast<const uint32_t*>(p.cache.k_pairs + pr);
+                pair_v = *reinterpret_cast<const uint32_t*>(p.cache.v_pairs + pr);
             }
         }
     };
     auto put = [&](uint32_t buf) {
+        if constexpr (kBits == 4) {
+            if (kCodeThreads >= kManyThreads || threadIdx.x < kCodeThreads) {
 #pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i) {
-            const uint32_t key = my_key + i * kRowsAtOnce;
-            u32x4 k, v;
-            if constexpr (kBits == 16) {
-                k = next_k[i], v = next_v[i];
-            } else {
-                k = decode8<E>(next_k[i][0], low16<E>(pair_k[i]), high16<E>(pair_k[i]));
-                v = decode8<E>(next_v[i][0], low16<E>(pair_v[i]), high16<E>(pair_v[i]));
+                for (uint32_t i = 0; i < 4; ++i) {
+                    lds_k[buf][code_key * kPieces + key_piece<D>(code_key, 4 * code_piece + i)] = decode8<E>(raw_k[i], low16<E>(pair_k), high16<E>(pair_k));
+                    lds_v[buf][code_key * kPieces + value_piece<D>(code_key, 4 * code_piece + i)] = decode8<E>(raw_v[i], low16<E>(pair_v), high16<E>(pair_v));
+                }
             }
-            if (!next_there[i]) v = u32x4{0, 0, 0, 0};
-            lds_k[buf][key_piece<D>(key, my_piece)] = k;
-            lds_v[buf][value_piece<D>(key, my_piece)] = v;
-            if (my_piece == 0) lds_seen[buf][key] = next_there[i];
         }
     };
 
-    places(first_tile);
-    fetch();
-    places(first_tile + 1);
+    // positions of the workgroup's first and last row
+    const int32_t all_first = seq.pos0 + (int32_t)uniform(over_group(p, row0)), all_last = seq.pos0 + (int32_t)uniform(over_group(p, row1));
+
+    if (threadIdx.x == 0) lds_strange = 0;
+    if (wave == 0) places(first_tile), put_places(0);
+    __syncthreads();
+    fetch(0);
+    if (wave == 0) places(first_tile + 1), put_places(1);
     put(0);
+    wait_loads();
     __syncthreads();
     for (uint32_t tile = first_tile; tile < last_tile; ++tile) {
         const uint32_t buf = (tile - first_tile) & 1u;
-        if (tile + 1 < last_tile) {
-            fetch();
-            places(tile + 2);
-        }
+        const uint64_t seen_all = lds_seen[(tile - first_tile) & 3u];
+        const uint32_t seen_lo = __builtin_amdgcn_readfirstlane((uint32_t)seen_all), seen_hi = __builtin_amdgcn_readfirstlane((uint32_t)(seen_all >> 32));
+        if (tile + 1 < last_tile) fetch(buf ^ 1u);
+        const bool mine = (tile & (kManyWaves - 1)) == wave;
+        if (mine) places(tile + 2);
         int32_t base, end;
         tile_at<kManyKeys>(sp, tile, base, end);
-        if (base <= pos_last) {                             // otherwise all of it lies after the wavefront's rows
-            f32x16 sc[2];
+        const bool sink_part = tile < sp.sink_tiles;
+        // Where not all rows see all keys, a NaN or infinity among the values must not reach the others as 0 * NaN: the rows
+        // that see it take it as it is (a weight does not change it), and zero stands in for it.
+        if (base + (int32_t)kManyKeys - 1 > all_first || (p.window && !sink_part && (int64_t)base <= (int64_t)all_last - p.window)) {
+            constexpr uint32_t kMine = kManyKeys * kPieces / kManyThreads;
+            uint32_t bad = 0;                               // the exponent, all ones, carries into the sign's place
 #pragma unroll
-            for (uint32_t t = 0; t < 2; ++t) {
+            for (uint32_t i = 0; i < kMine; ++i) {
+                const u32x4 x = lds_v[buf][i * kManyThreads + threadIdx.x];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sc[t][j] = 0.0f;
-#pragma unroll
-                for (uint32_t i = 0; i < kSteps; ++i) sc[t] = mfma32<E>(lds_k[buf][key_piece<D>(32 * t + col, 2 * i + half)], q[i], sc[t]);
+                for (int j = 0; j < 4; ++j) bad |= (x[j] & 0x7FFF7FFFu) + kExponentStep<E>;
             }
-            // what is not seen: keys that are not there (any row), keys after a row or before its window
-            const uint64_t seen = __ballot(lds_seen[buf][lane] != 0);
-            const bool sink_part = tile < sp.sink_tiles;
-            const bool each = base + (int32_t)kManyKeys - 1 > pos_first || (p.window && !sink_part && (int64_t)base <= (int64_t)pos_last - p.window);
-            uint32_t shows = 0xFFFFFFFFu;                   // one bit a register: the row sees the key
-            if (each || seen != ~0ull) {
+            if (bad & 0x80008000u) lds_strange = tile + 1;
+            __syncthreads();
+            if (uniform(lds_strange) == tile + 1) {
+#pragma unroll 1
+                for (uint32_t k = 0; k < kManyKeys; ++k) {
+                    const int32_t key = base + (int32_t)k;
+                    const bool there = ((k < 32 ? seen_lo >> k : seen_hi >> (k - 32)) & 1u) != 0;
+                    const bool sight = there && key <= pos && (key > behind || (uint32_t)key < p.sinks);
 #pragma unroll
-                for (uint32_t t = 0; t < 2; ++t)
+                    for (uint32_t i = 0; i < kOut; ++i)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const uint32_t at = 32 * t + (j / 4) * 8 + 4 * half + j % 4;
-                        const int32_t key = base + (int32_t)at;
-                        const bool sight = ((seen >> at) & 1u) && key <= pos &&
-                                           (!p.window || (int64_t)key > (int64_t)pos - p.window || (uint32_t)key < p.sinks);
-                        if (!sight) shows &= ~(1u << (16 * t + j)), sc[t][j] = -INFINITY;
+                        for (int j = 0; j < 16; ++j) {
+                            const uint32_t c = 32 * i + (j / 4) * 8 + 4 * half + j % 4;
+                            const uint32_t x = reinterpret_cast<const uint16_t*>(lds_v[buf])[(k * kPieces + value_piece<D>(k, c / 8)) * 8 + c % 8];
+                            if (sight && (x & kExponent<E>) == kExponent<E>) o[i][j] += low16<E>(x);
+                        }
+                }
+                __syncthreads();
+#pragma unroll 1
+                for (uint32_t i = 0; i < kMine; ++i) {
+                    u32x4 x = lds_v[buf][i * kManyThreads + threadIdx.x];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if ((x[j] & kExponent<E>) == kExponent<E>) x[j] &= 0xFFFF0000u;
+                        if ((x[j] >> 16 & kExponent<E>) == kExponent<E>) x[j] &= 0xFFFFu;
                     }
+                    lds_v[buf][i * kManyThreads + threadIdx.x] = x;
+                }
+                __syncthreads();
             }
-            float top = -INFINITY;
+        }
+        // work, unless all of the tile lies after the wavefront's rows or before their windows
+        if (base <= pos_last && !(p.window && !sink_part && (uint32_t)base >= p.sinks && (int64_t)base + kManyKeys - 1 <= (int64_t)pos_first - p.window)) {
+            const char* const keys = reinterpret_cast<const char*>(lds_k[buf]);
+            const char* const values = reinterpret_cast<const char*>(lds_v[buf]);
+            f32x16 sc[2];
 #pragma unroll
             for (uint32_t t = 0; t < 2; ++t)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) top = fmaxf(top, sc[t][j]);
+                for (int j = 0; j < 16; ++j) sc[t][j] = 0.0f;
+            // pieces are told apart by exclusive or, so one number and the product's give the place
+            const uint32_t key_at = here(col * (2 * D) + key_piece<D>(col, half) * 16);
+#pragma unroll
+            for (uint32_t i = 0; i < kSteps; ++i)
+#pragma unroll
+                for (uint32_t t = 0; t < 2; ++t)
+                    sc[t] = mfma32<E>(*reinterpret_cast<const u32x4*>(keys + 32 * t * (2 * D) + (key_at ^ (32 * i))), q[i], sc[t]);
+            // six operands are read ahead of the products
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+            for (uint32_t i = 0; i < 2 * kSteps - 6; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
+
+            // what is not seen: keys that are not there (any row), keys after a row or before its window
+            const bool each = base + (int32_t)kManyKeys - 1 > pos_first || (p.window && !sink_part && (int64_t)base <= (int64_t)pos_last - p.window);
+            if (each || (seen_lo & seen_hi) != ~0u) {
+#pragma unroll
+                for (uint32_t t = 0; t < 2; ++t) {
+                    // register j has key 8 (j / 4) + j % 4 from here on; bit j of each number says so of it
+                    const int32_t key0 = base + (int32_t)(32 * t + 4 * half);
+                    const uint32_t there = (t ? seen_hi : seen_lo) >> (4 * half);
+                    uint32_t shows = (there & 15u) | (there >> 4 & 0xF0u) | (there >> 8 & 0xF00u) | (there >> 12 & 0xF000u);
+                    auto below = [&](int64_t n) {           // registers whose key is below key0 + n
+                        const uint32_t x = (uint32_t)min(max(n, (int64_t)0), (int64_t)32);
+                        return (1u << (4 * (x / 8) + min(x % 8, 4u))) - 1u;
+                    };
+                    shows &= below((int64_t)pos - key0 + 1);
+                    shows &= ~below((int64_t)behind - key0 + 1) | below((int64_t)p.sinks - key0);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sc[t][j] = (shows >> j) & 1u ? sc[t][j] : -INFINITY;
+                }
+            }
+            float top = sc[0][0];
+#pragma unroll
+            for (int j = 1; j < 32; ++j) top = fmaxf(top, sc[j / 16][j % 16]);
             top = max_halves(top) * p.scale_log2;
             const bool raise = top > m + kHeadroom || (m == -INFINITY && top > m);
             if (__any(raise)) {
-                const float grown = raise ? top : m, keep = raise ? exp2_of(m - grown) : 1.0f;
+                const float grown = raise ? top : m, keep = raise && m != -INFINITY ? exp2_of(m - grown) : 1.0f;
                 m = grown;
                 l *= keep;
 #pragma unroll
@@ -205,70 +293,38 @@ __global__ __launch_bounds__(kManyThreads, 2) void k_attend_many(const AttnParam
                     w[2 * t + j / 8][j % 8 / 2] = pack2<E>(a, b);
                 }
             const uint32_t key_in = 4 * half + (lane % 16) / 4, piece_in = ((lane / 16) % 2) * 2 + (lane % 4) / 2, byte_in = (lane % 2) * 8;
-            uint32_t strange = 0;                           // one bit an operand that holds a NaN or an infinity
+            const uint32_t value_at = here(key_in * (2 * D) + value_piece<D>(key_in, piece_in) * 16 + byte_in);
 #pragma unroll
-            for (uint32_t i = 0; i < kOut; ++i)
+            for (uint32_t t = 0; t < 4; ++t)                // channels 32 i .. of keys 16 t ..
 #pragma unroll
-                for (uint32_t t = 0; t < 4; ++t) {
-                    const char* at = reinterpret_cast<const char*>(lds_v[buf]);
-                    const u32x2 lo = lds_transposed(at + value_piece<D>(16 * t + key_in, 4 * i + piece_in) * 16 + byte_in);
-                    const u32x2 hi = lds_transposed(at + value_piece<D>(16 * t + 8 + key_in, 4 * i + piece_in) * 16 + byte_in);
-                    const u32x4 a = {lo[0], lo[1], hi[0], hi[1]};
-                    if (each) {                             // one that not all rows see must not reach the others as 0 * NaN
-                        bool bad = false;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) bad |= not_finite16(a[j], kExponent<E>);
-                        if (__any(bad)) {
-                            strange |= 1u << (4 * i + t);
-                            continue;
-                        }
-                    }
-                    o[i] = mfma32<E>(a, w[t], o[i]);
+                for (uint32_t i = 0; i < kOut; ++i) {
+                    const char* at = values + (value_at ^ (64 * i));
+                    const u32x2 lo = lds_transposed(at + 16 * t * (2 * D)), hi = lds_transposed(at + (16 * t + 8) * (2 * D));
+                    o[i] = mfma32<E>(u32x4{lo[0], lo[1], hi[0], hi[1]}, w[t], o[i]);
                 }
-            if (strange) {                                  // rare: those 32 channels of those 16 keys, each row with the keys that it sees
-#pragma unroll
-                for (uint32_t i = 0; i < kOut; ++i)
-#pragma unroll 1
-                    for (uint32_t t = 0; t < 4; ++t) {
-                        if (!((strange >> (4 * i + t)) & 1u)) continue;
-#pragma unroll 1
-                        for (uint32_t k = 0; k < 16; ++k) {
-                            // key 16 t + k is in the lanes of half (k / 4) % 2, in register 8 (t % 2) + 4 (k / 8) + k % 4 of tile t / 2
-                            const uint32_t reg = 16 * (t / 2) + 8 * (t % 2) + 4 * (k / 8) + k % 4, from_lane = (k / 4) % 2 * 32 + col;
-                            const u32x4 ws = t == 0 ? w[0] : t == 1 ? w[1] : t == 2 ? w[2] : w[3];
-                            const uint32_t two = reg % 8 / 2 == 0 ? ws[0] : reg % 8 / 2 == 1 ? ws[1] : reg % 8 / 2 == 2 ? ws[2] : ws[3];
-                            const uint32_t two_in = __shfl(two, from_lane);
-                            const bool sees = (__shfl(shows, from_lane) >> reg) & 1u;
-                            const float weight = reg % 2 ? high16<E>(two_in) : low16<E>(two_in);
-                            const uint32_t key = 16 * t + k;
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                const uint32_t ch = 32 * i + (j / 4) * 8 + 4 * half + j % 4;
-                                const uint16_t x = reinterpret_cast<const uint16_t*>(lds_v[buf])[value_piece<D>(key, ch / 8) * 8 + ch % 8];
-                                if (sees) o[i][j] += weight * low16<E>(x);
-                            }
-                        }
-                    }
-            }
         }
         if (tile + 1 < last_tile) put(buf ^ 1u);
+        if (mine) put_places(tile - first_tile + 2);
+        wait_loads();
         __syncthreads();
     }
 
     const float total = sum_halves(l);
-    if (row0 + wave * 32 + col >= rows) return;
+    const uint32_t row = row0 + wave * 32 + here(col);
     if (alone) {
+        // the halves of the wavefront have 4 channels each of every 8: they change every other 4, so that each has 8 in a row
         const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-        char* dst = p.out.data + (int64_t)(seq.first + (int32_t)token) * p.out.token_stride + (int64_t)q_head * p.out.head_stride;
+        char* dst = p.out.data + (int64_t)(seq.first + (int32_t)token) * p.out.token_stride + (int64_t)(head * p.group + r - token * p.group) * p.out.head_stride + 16 * half;
 #pragma unroll
         for (uint32_t i = 0; i < kOut; ++i)
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-                const u32x2 x = {pack2<E>(o[i][j] * inv, o[i][j + 1] * inv), pack2<E>(o[i][j + 2] * inv, o[i][j + 3] * inv)};
-                *reinterpret_cast<u32x2*>(dst + 2 * (32 * i + 2 * j + 4 * half)) = x;
+            for (int j = 0; j < 16; j += 8) {
+                const auto a = __builtin_amdgcn_permlane32_swap(pack2<E>(o[i][j] * inv, o[i][j + 1] * inv), pack2<E>(o[i][j + 4] * inv, o[i][j + 5] * inv), false, false);
+                const auto b = __builtin_amdgcn_permlane32_swap(pack2<E>(o[i][j + 2] * inv, o[i][j + 3] * inv), pack2<E>(o[i][j + 6] * inv, o[i][j + 7] * inv), false, false);
+                if (row < rows) *reinterpret_cast<u32x4*>(dst + 2 * (32 * i + 2 * j)) = u32x4{a[0], b[0], a[1], b[1]};
             }
-    } else {
-        const uint64_t at = ((uint64_t)z * p.batch.n_tokens + (uint32_t)(seq.first + (int32_t)token)) * p.q_heads + q_head;
+    } else if (row < rows) {
+        const uint64_t at = ((uint64_t)z * p.batch.n_tokens + (uint32_t)(seq.first + (int32_t)token)) * p.q_heads + head * p.group + r - token * p.group;
 #pragma unroll
         for (uint32_t i = 0; i < kOut; ++i)
 #pragma unroll

@@ -9,7 +9,8 @@ namespace {
 
 constexpr uint32_t kFewKeys = 32;        // keys that a wavefront of the kernel of few rows takes at a time
 constexpr uint32_t kManyKeys = 64;       // keys that a workgroup of the kernel of many rows takes at a time
-constexpr uint32_t kManyRows = 128;      // rows of such a workgroup
+constexpr uint32_t kManyWaves = 4, kManyThreads = kManyWaves * kLanes;
+constexpr uint32_t kManyRows = 32 * kManyWaves;   // rows of such a workgroup
 
 struct AttnParams {
     Cache cache;
@@ -73,6 +74,7 @@ __device__ __forceinline__ u32x2 lds_transposed(const char* at) {
 __device__ __forceinline__ bool not_finite16(uint32_t two, uint32_t exponent) {
     return (two & exponent) == exponent || ((two >> 16) & exponent) == exponent;
 }
+template <typename E> constexpr uint32_t kExponentStep = std::is_same_v<E, bf16> ? 0x00800080u : 0x04000400u;   // 1 in both exponents of a dword
 template <typename E> constexpr uint32_t kExponent = std::is_same_v<E, bf16> ? 0x7F80u : 0x7C00u;
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126: 0
