@@ -82,18 +82,24 @@ struct Plan {
     bool few, many;
     uint32_t few_tiles;                  // tiles of 16 rows
     uint32_t few_rows, few_stride, few_groups, few_seqs;
+    bool few_team;                       // a workgroup for each (sequence, kv head)
     uint32_t many_chunk, many_chunks, row_tiles;
     uint64_t few_n, many_n;              // rows of results in the workspace
     uint64_t plan_bytes, bytes;
 };
 
-constexpr uint32_t kResident = 512;      // workgroups that the chip holds of either kernel: two on each of 256 CUs
+constexpr uint32_t kResident = 512;      // workgroups that the chip holds of the kernels: two on each of 256 CUs (one where rows need all registers)
 
-// Short sequences are not split (a wavefront takes a whole sequence and head, and nothing is left to join): the join costs
-// about 4 us, a tile of a wavefront on its own about 1.1 us.  32 heads on 8, 128 channels, bf16, us whole / split and joined:
-// 8 sequences of 64 keys 7.1 / 10.9, of 128 9.3 / 11.0, of 192 11.5 / 11.4, of 256 13.8 / 11.9; with 64 sequences, whose 512
-// pieces fill half the chip, of 256 16.8 / 20.9 (4 bits 16.2 / 17.9), of 512 34.5 / 36.6 (4 bits 25.7 / 20.9).
-constexpr uint32_t kUnsplitTiles = 5, kUnsplitTilesOfMany = 8, kManyPairs = 512;
+// How the kernel of few rows deals out its work.  32 heads on 8, 128 channels, bf16, sequences of one length, us:
+//  - A team for each (sequence, head) while these are fewer than the chip's 256 CUs, and not so long that a ragged batch,
+//    which takes as long as its longest, would wait for one.  Team / line: 8 sequences of 256 keys 7.1 / 11.8, of 512
+//    9.4 / 13.2, of 1024 12.8 / 17.5, of 4096 48 / 37; 32 sequences of 512 14.8 / 21.2 (of 256 about 14 on the line).
+//  - Otherwise short sequences go uncut to a wavefront each, so that nothing is left to join (which costs about 5 us, a tile
+//    of a wavefront on its own about 1.1 us).  Uncut / line / team: 64 sequences of 128 keys 11.8 / 16.2 / 14.3, of 256
+//    16.8 / 20.9 / -, of 512 34.5 / 36.6 / 32.2 (4 bits 25.7 / 20.9 / 19.7).
+//  - Otherwise the line: each wavefront an equal piece.
+constexpr uint32_t kTeamPairs = 256, kTeamTiles = 16, kTeamTilesOfFew = 32, kFewPairs = 128;
+constexpr uint32_t kUncutTiles = 5, kUncutTilesOfMany = 8, kManyPairs = 512;
 constexpr uint32_t kFewLeast = 2;        // places of the line that a wavefront of the kernel of few rows takes at least
 
 ap_status plan_of(const ap_kv_cache* c, const Batch& b, uint32_t q_heads, uint32_t window, uint32_t sinks, Plan* out) {
@@ -114,12 +120,14 @@ ap_status plan_of(const ap_kv_cache* c, const Batch& b, uint32_t q_heads, uint32
         r.few_seqs = std::min(b.n_seqs, kFewSeqs);
         const uint64_t pairs = (uint64_t)r.few_seqs * c->kv_heads, units = pairs * ((uint64_t)tiles + kFewEnter);
         if (units >= kMost || pairs * r.few_stride >= kMostGroups) return AP_ERR_RANGE;
-        if (tiles <= (pairs >= kManyPairs ? kUnsplitTilesOfMany : kUnsplitTiles)) {
-            r.few_groups = (uint32_t)((pairs + kFewWaves - 1) / kFewWaves);
+        if (pairs <= kTeamPairs && tiles <= (pairs <= kFewPairs ? kTeamTilesOfFew : kTeamTiles)) {
+            r.few_team = true;
+        } else if (tiles <= (pairs >= kManyPairs ? kUncutTilesOfMany : kUncutTiles)) {
+            r.few_groups = (uint32_t)((pairs + kLineWaves - 1) / kLineWaves);
         } else {
-            r.few_groups = (uint32_t)std::min<uint64_t>((units + kFewWaves - 1) / kFewWaves, kResident);
+            r.few_groups = (uint32_t)std::min<uint64_t>((units + kLineWaves - 1) / kLineWaves, r.few_tiles == 2 && c->head_dim == 128 ? kResident / 2 : kResident);
             r.plan_bytes = (4ull * (r.few_seqs + 2) + 15) / 16 * 16;
-            r.few_n = 2ull * r.few_groups * kFewWaves * r.few_stride;
+            r.few_n = 2ull * r.few_groups * kLineWaves * r.few_stride;
         }
     }
     if (r.many) {
@@ -230,7 +238,7 @@ ap_status ap_attention(const ap_kv_cache* cache, const ap_seq_batch* batch, cons
     p.window = window, p.sinks = window ? sinks : 0;
     p.scale_log2 = scale * 1.44269504088896341f;
     p.few_rows = plan.few ? plan.few_rows : 0, p.few_stride = plan.few_stride;
-    p.few_waves = plan.few_groups * kFewWaves, p.few_least = kFewLeast, p.many_chunk = plan.many_chunk;
+    p.few_waves = plan.few_groups * kLineWaves, p.few_least = kFewLeast, p.many_chunk = plan.many_chunk;
     char* space = (char*)workspace;
     p.few_plan = plan.plan_bytes ? (uint32_t*)space : nullptr;
     p.few_o = (float*)(space + plan.plan_bytes), p.many_o = p.few_o + plan.few_n * cache->head_dim;
@@ -239,13 +247,15 @@ ap_status ap_attention(const ap_kv_cache* cache, const ap_seq_batch* batch, cons
     for_cache(cache, [&](auto e, auto d, auto b) {
         using E = decltype(e);
         if (plan.few) {
-            auto kernel = plan.few_tiles == 1 ? k_attend_few<E, d(), b(), 1> : k_attend_few<E, d(), b(), 2>;
+            auto kernel = plan.few_team ? (plan.few_tiles == 1 ? k_attend_few<E, d(), b(), 1, true> : k_attend_few<E, d(), b(), 2, true>)
+                                        : (plan.few_tiles == 1 ? k_attend_few<E, d(), b(), 1, false> : k_attend_few<E, d(), b(), 2, false>);
+            const uint32_t waves = !plan.few_team ? kLineWaves : plan.few_tiles == 1 ? kFewWaves<d(), b(), 1, true> : kFewWaves<d(), b(), 2, true>;
             for (uint32_t s = 0; s < batch->n_seqs; s += kFewSeqs) {    // so many sequences a launch, one launch after the other in one workspace
                 AttnParams x = p;
                 x.batch.n_seqs = std::min(kFewSeqs, batch->n_seqs - s);
                 x.batch.first += s, x.batch.kv_len += s, x.batch.table += (int64_t)s * p.batch.table_stride;
                 const uint32_t pairs = x.batch.n_seqs * p.kv_heads;
-                hipLaunchKernelGGL(kernel, dim3(plan.few_groups), dim3(kFewThreads), 0, on, x);
+                hipLaunchKernelGGL(kernel, dim3(plan.few_team ? pairs : plan.few_groups), dim3(waves * kLanes), 0, on, x);
                 if (p.few_plan) hipLaunchKernelGGL((k_join_few<E, d()>), dim3((pairs * plan.few_stride + 3) / 4), dim3(256), 0, on, x);
             }
         }

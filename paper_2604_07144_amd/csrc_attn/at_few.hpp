@@ -8,7 +8,8 @@
 // 4 * D bytes (16 bits) against 4 * D * rows operations.  What follows from it:
 //  - Work is dealt out evenly whatever the lengths: the tiles (32 keys) of all sequences and heads are one line, and each
 //    of a fixed number of wavefronts takes an equal piece of it, which may begin and end inside a sequence.  Every
-//    workgroup works the line out from the lengths on the device.
+//    workgroup works the line out from the lengths on the device; a second kernel joins what was cut.
+//    Few and short sequences are not cut: eight wavefronts share each (sequence, head) and join their parts in LDS.
 //  - Wavefronts go their own way, without a barrier, and have the next 32 keys and values on their way to registers while
 //    they work on the present ones.  Loads take whole rows, 16 bytes a lane; the exchange into the operand layouts of the
 //    matrix units is LDS's, which has bandwidth to spare here.
@@ -27,7 +28,7 @@
 
 namespace {
 
-constexpr uint32_t kFewWaves = 4, kFewThreads = kFewWaves * kLanes;
+constexpr uint32_t kLineWaves = 4, kLineThreads = kLineWaves * kLanes;   // of a workgroup that works on the line
 constexpr uint32_t kFewRows = 32;        // most rows (new tokens times shared heads) of the kernel
 constexpr uint32_t kFewSeqs = 256;       // most sequences of a launch (a thread each): the line of their tiles stands in LDS
 constexpr uint32_t kFewEnter = 3;        // what beginning with a sequence costs a wavefront, in tiles
@@ -72,9 +73,14 @@ struct FewSeq {
     Span span;
 };
 
-// kTiles: tiles of 16 rows.
-template <typename E, uint32_t D, uint32_t kBits, uint32_t kTiles>
-__global__ __launch_bounds__(kFewThreads, kTiles == 2 && kBits == 16 && D == 128 ? 1 : 2) void k_attend_few(const AttnParams p) {
+// Wavefronts of a workgroup: a team, which shares a (sequence, head), has 8 where registers allow two on a SIMD.
+template <uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
+constexpr uint32_t kFewWaves = kTeam && !(D == 128 && kBits == 16 && kTiles == 2) ? 8 : 4;
+
+// kTiles: tiles of 16 rows.  kTeam: a workgroup takes a (sequence, head) and joins its wavefronts' parts itself.
+template <typename E, uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
+__global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTiles == 2 && D == 128 && (kBits == 16 || !kTeam) ? 1 : 2)) void k_attend_few(const AttnParams p) {
+    constexpr uint32_t kWaves = kFewWaves<D, kBits, kTiles, kTeam>;
     constexpr bool kCodes = kBits == 4;
     constexpr uint32_t kGroups = D / 64;
     constexpr uint32_t kSteps = D / 32, kOut = D / 16;      // products over channels; tiles of 16 channels of the result
@@ -83,59 +89,64 @@ __global__ __launch_bounds__(kFewThreads, kTiles == 2 && kBits == 16 && D == 128
     constexpr uint32_t kRowsAtOnce = kLanes / kLaneRows, kLoads = kFewKeys / kRowsAtOnce;
     constexpr uint32_t kPairFloats = 2 * kGroups;           // (step, lo) of a key
     constexpr uint32_t kWaveBytes = 2 * kSideBytes + (kCodes ? 2 * kFewKeys * kPairFloats * 4 : 0);
-    __shared__ __attribute__((aligned(16))) char lds[kFewWaves * kWaveBytes];
-    __shared__ int64_t lds_rows[kFewWaves][kFewKeys];
-    __shared__ uint32_t lds_line[kFewSeqs + 1], lds_sum[kFewWaves];
-    __shared__ FewSeq lds_seq[kFewSeqs];
-    static_assert(kFewSeqs == kFewThreads);
+    constexpr uint32_t kOutStride = D + 4;                  // floats between rows where a team's results meet
+    constexpr uint32_t kJoinBytes = kTeam ? 16 * kOutStride * 4 : 0;
+    __shared__ __attribute__((aligned(16))) char lds[kWaves * (kWaveBytes > kJoinBytes ? kWaveBytes : kJoinBytes)];
+    __shared__ int64_t lds_rows[kWaves][kFewKeys];
+    __shared__ uint32_t lds_line[kTeam ? 1 : kFewSeqs + 1], lds_sum[kWaves];
+    __shared__ FewSeq lds_seq[kTeam ? 1 : kFewSeqs];
+    __shared__ float lds_m[kTeam ? kWaves : 1][16], lds_l[kTeam ? kWaves : 1][16];
+    static_assert(kFewSeqs == kLineThreads);
 
     const uint32_t lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes), col = lane % 16, quad = lane / 16;
 
-    // The line: a sequence has, for each head, kFewEnter places for beginning with it and one for each tile; none where it
-    // is not this kernel's.  lds_line[s]: places of the sequences before s, for one head.
-    uint32_t mine = 0;
-    if (threadIdx.x < p.batch.n_seqs) {
-        const Seq seq = seq_at(p.batch, threadIdx.x);
-        const int32_t n_new = min(seq.n_new, (int32_t)p.batch.max_new);
-        const uint32_t rows = (uint32_t)n_new * p.group;
-        if (rows != 0 && rows <= p.few_rows) {
-            const Span sp = span_of<kFewKeys>(p, seq, 0, n_new - 1);
-            mine = sp.tiles + kFewEnter;
-            lds_seq[threadIdx.x] = FewSeq{seq.first, n_new, seq.pos0, sp};
+    const uint32_t worker = blockIdx.x * kWaves + wave;
+    uint32_t unit = 0, unit_end = 1;
+    if constexpr (!kTeam) {
+        // The line: a sequence has, for each head, kFewEnter places for beginning with it and one for each tile; none where it
+        // is not this kernel's.  lds_line[s]: places of the sequences before s, for one head.
+        uint32_t mine = 0;
+        if (threadIdx.x < p.batch.n_seqs) {
+            const Seq seq = seq_at(p.batch, threadIdx.x);
+            const int32_t n_new = min(seq.n_new, (int32_t)p.batch.max_new);
+            const uint32_t rows = (uint32_t)n_new * p.group;
+            if (rows != 0 && rows <= p.few_rows) {
+                const Span sp = span_of<kFewKeys>(p, seq, 0, n_new - 1);
+                mine = sp.tiles + kFewEnter;
+                lds_seq[threadIdx.x] = FewSeq{seq.first, n_new, seq.pos0, sp};
+            }
         }
-    }
-    uint32_t upto = mine;
+        uint32_t upto = mine;
 #pragma unroll
-    for (uint32_t m = 1; m < kLanes; m *= 2) {
-        const uint32_t other = __shfl_up(upto, m);
-        if (lane >= m) upto += other;
+        for (uint32_t m = 1; m < kLanes; m *= 2) {
+            const uint32_t other = __shfl_up(upto, m);
+            if (lane >= m) upto += other;
+        }
+        if (lane == kLanes - 1) lds_sum[wave] = upto;
+        __syncthreads();
+        uint32_t total = 0;
+        for (uint32_t w = 0; w < kWaves; ++w) {
+            if (w < wave) upto += lds_sum[w];
+            total += lds_sum[w];
+        }
+        lds_line[threadIdx.x + 1] = upto;
+        if (threadIdx.x == 0) lds_line[0] = 0;
+        __syncthreads();
+        const uint32_t units = total * p.kv_heads, per = max(p.few_least, (units + p.few_waves - 1) / p.few_waves);
+        if (p.few_plan && blockIdx.x == 0) {                                  // for the kernel that joins
+            if (threadIdx.x < p.batch.n_seqs) p.few_plan[2 + threadIdx.x] = upto;
+            if (threadIdx.x == 0) p.few_plan[0] = per, p.few_plan[1] = 0;
+        }
+        if (p.few_plan) {
+            unit = min(worker * per, units), unit_end = min(unit + per, units);
+        } else {                                                // no split: each worker has a (sequence, head)
+            const uint32_t s = worker / p.kv_heads;
+            if (s >= p.batch.n_seqs) return;
+            const uint32_t of_head = lds_line[s + 1] - lds_line[s];
+            unit = lds_line[s] * p.kv_heads + (worker - s * p.kv_heads) * of_head, unit_end = unit + of_head;
+        }
+        unit = __builtin_amdgcn_readfirstlane(unit), unit_end = __builtin_amdgcn_readfirstlane(unit_end);
     }
-    if (lane == kLanes - 1) lds_sum[wave] = upto;
-    __syncthreads();
-    uint32_t total = 0;
-    for (uint32_t w = 0; w < kFewWaves; ++w) {
-        if (w < wave) upto += lds_sum[w];
-        total += lds_sum[w];
-    }
-    lds_line[threadIdx.x + 1] = upto;
-    if (threadIdx.x == 0) lds_line[0] = 0;
-    __syncthreads();
-    const uint32_t units = total * p.kv_heads, per = max(p.few_least, (units + p.few_waves - 1) / p.few_waves);
-    if (p.few_plan && blockIdx.x == 0) {                                  // for the kernel that joins
-        if (threadIdx.x < p.batch.n_seqs) p.few_plan[2 + threadIdx.x] = upto;
-        if (threadIdx.x == 0) p.few_plan[0] = per, p.few_plan[1] = 0;
-    }
-    const uint32_t worker = blockIdx.x * kFewWaves + wave;
-    uint32_t unit, unit_end;
-    if (p.few_plan) {
-        unit = min(worker * per, units), unit_end = min(unit + per, units);
-    } else {                                                // no split: each worker has a (sequence, head)
-        const uint32_t s = worker / p.kv_heads;
-        if (s >= p.batch.n_seqs) return;
-        const uint32_t of_head = lds_line[s + 1] - lds_line[s];
-        unit = lds_line[s] * p.kv_heads + (worker - s * p.kv_heads) * of_head, unit_end = unit + of_head;
-    }
-    unit = __builtin_amdgcn_readfirstlane(unit), unit_end = __builtin_amdgcn_readfirstlane(unit_end);
 
     // where the lane's 16 bytes of load i lie: row i * kRowsAtOnce + lane / kLaneRows, piece lane % kLaneRows
     const uint32_t load_row = lane / kLaneRows, load_piece = lane % kLaneRows;
@@ -154,26 +165,38 @@ __global__ __launch_bounds__(kFewThreads, kTiles == 2 && kBits == 16 && D == 128
     };
 
     while (unit < unit_end) {
-        // the piece of the line: the last sequence whose tiles begin at or before the unit, its head, tiles
-        uint32_t s = 0, s_end = p.batch.n_seqs;
-        while (s_end - s > 1) {
-            const uint32_t mid = (s + s_end) / 2;
-            if (__builtin_amdgcn_readfirstlane(lds_line[mid]) * p.kv_heads <= unit) s = mid;
-            else s_end = mid;
+        // the piece of the line: the last sequence whose tiles begin at or before the unit, its head, tiles; a team's wavefronts
+        // take every kWaves-th tile of theirs
+        uint32_t s, head, first_tile, last_tile, tiles;
+        FewSeq its;
+        if constexpr (kTeam) {
+            s = blockIdx.x / p.kv_heads, head = blockIdx.x - s * p.kv_heads;
+            const Seq seq = seq_at(p.batch, s);
+            its.first = seq.first, its.n_new = min(seq.n_new, (int32_t)p.batch.max_new), its.pos0 = seq.pos0;
+            if (its.n_new == 0 || (uint32_t)its.n_new * p.group > p.few_rows) return;
+            its.span = span_of<kFewKeys>(p, seq, 0, its.n_new - 1);
+            tiles = uniform(its.span.tiles), first_tile = wave, last_tile = tiles;
+            unit = unit_end;
+        } else {
+            s = 0;
+            for (uint32_t s_end = p.batch.n_seqs; s_end - s > 1;) {
+                const uint32_t mid = (s + s_end) / 2;
+                if (uniform(lds_line[mid]) * p.kv_heads <= unit) s = mid;
+                else s_end = mid;
+            }
+            const uint32_t line = uniform(lds_line[s]), of_head = uniform(lds_line[s + 1]) - line, at_line = unit - line * p.kv_heads;
+            head = at_line / of_head;
+            const uint32_t place = at_line - head * of_head, n_units = min(of_head - place, unit_end - unit);
+            tiles = of_head - kFewEnter, first_tile = max(place, kFewEnter) - kFewEnter, last_tile = max(place + n_units, kFewEnter) - kFewEnter;
+            unit += n_units;
+            if (first_tile == last_tile && (tiles || place)) continue;   // the beginning alone, which the next worker has too
+            its = lds_seq[s];
         }
-        const uint32_t line = __builtin_amdgcn_readfirstlane(lds_line[s]), of_head = __builtin_amdgcn_readfirstlane(lds_line[s + 1]) - line;
-        const uint32_t at_line = unit - line * p.kv_heads, head = at_line / of_head, place = at_line - head * of_head;
-        const uint32_t n_units = min(of_head - place, unit_end - unit), tiles = of_head - kFewEnter;
-        const uint32_t first_tile = max(place, kFewEnter) - kFewEnter, last_tile = max(place + n_units, kFewEnter) - kFewEnter;
-        unit += n_units;
-        if (first_tile == last_tile && (tiles || place)) continue;       // the beginning alone, which the next worker has too
-        const FewSeq& its = lds_seq[s];
-        const int32_t seq_first = __builtin_amdgcn_readfirstlane(its.first), n_new = __builtin_amdgcn_readfirstlane(its.n_new);
-        const int32_t pos_first = __builtin_amdgcn_readfirstlane(its.pos0), pos_last = pos_first + n_new - 1;
+        const int32_t seq_first = uniform(its.first), n_new = uniform(its.n_new), pos_first = uniform(its.pos0), pos_last = pos_first + n_new - 1;
         const uint32_t rows = (uint32_t)n_new * p.group;
         Span sp;
-        sp.sink_end = __builtin_amdgcn_readfirstlane(its.span.sink_end), sp.begin = __builtin_amdgcn_readfirstlane(its.span.begin);
-        sp.end = __builtin_amdgcn_readfirstlane(its.span.end), sp.sink_tiles = __builtin_amdgcn_readfirstlane(its.span.sink_tiles);
+        sp.sink_end = uniform(its.span.sink_end), sp.begin = uniform(its.span.begin), sp.end = uniform(its.span.end), sp.sink_tiles = uniform(its.span.sink_tiles);
+        constexpr uint32_t kStep = kTeam ? kWaves : 1;
 
         // ---- what is fetched: places of a tile's keys (lane % 32 has a key), then its rows
         const int32_t* table = p.batch.table + (int64_t)s * p.batch.table_stride;
@@ -207,7 +230,7 @@ __global__ __launch_bounds__(kFewThreads, kTiles == 2 && kBits == 16 && D == 128
         };
         places(first_tile);
         fetch();
-        places(first_tile + 1);
+        places(first_tile + kStep);
 
         // ---- queries as the second operand: column = row of the result.  Product i takes channels 32 i + 8 quad + 0..7; in
         // 4 bits, of each 64, first the codes of 8 bytes' first dwords, then of the second: byte 8 quad + 4 (i % 2), with the
@@ -269,7 +292,7 @@ __global__ __launch_bounds__(kFewThreads, kTiles == 2 && kBits == 16 && D == 128
             for (uint32_t g = 0; g < kGroups; ++g) eights[n][g] = f32x4{0, 0, 0, 0}, lows[n][g] = 0.0f;
         }
 
-        for (uint32_t tile = first_tile; tile < last_tile; ++tile) {
+        for (uint32_t tile = first_tile; tile < last_tile; tile += kStep) {
             const uint32_t seen = seen_next;
             // rows to LDS; values (in 4 bits: pairs) that are not there as zeros
             if (!kCodes && seen != ~0u) {
@@ -320,7 +343,7 @@ __global__ __launch_bounds__(kFewThreads, kTiles == 2 && kBits == 16 && D == 128
                 else *reinterpret_cast<f32x2*>(to) = f32x2{par[0], par[1]};
             }
             fetch();
-            places(tile + 2);
+            places(tile + 2 * kStep);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             int32_t base, end;
             tile_at<kFewKeys>(sp, tile, base, end);
@@ -506,28 +529,21 @@ __global__ __launch_bounds__(kFewThreads, kTiles == 2 && kBits == 16 && D == 128
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
 
-        // ---- the piece's rows: finished where it has all of the sequence's tiles, otherwise to the workspace
-        const bool whole = last_tile - first_tile == tiles;
+        // ---- the piece's rows: a team's wavefronts meet in LDS; otherwise finished where all of the sequence's tiles are here,
+        // and to the workspace where not
+        const bool whole = kTeam || last_tile - first_tile == tiles;
         const uint32_t slot = 2 * worker + (first_tile ? 0u : 1u);
 #pragma unroll
         for (uint32_t n = 0; n < kTiles; ++n) {
             const uint32_t row = n * 16 + here(col), quad = here(lane) / 16;
             const float sum = sum_column(l[n]);
-            float f = whole ? (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) : 1.0f, low[kGroups];
+            float f = !kTeam && whole ? (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) : 1.0f, low[kGroups];
             if constexpr (kCodes) {
 #pragma unroll
                 for (uint32_t g = 0; g < kGroups; ++g) low[g] = sum_column(lows[n][g]) * f;
                 f *= power2(kCodeExponent<E> - kOperandExponent<E> + step_exp);
             }
-            if (row < rows) {
-                const uint32_t token = over_group(p, row);
-                const uint64_t at = (uint64_t)slot * p.few_stride + row;
-                char* const dst = p.out.data + (int64_t)(seq_first + (int32_t)token) * p.out.token_stride + (int64_t)(head * p.group + row - token * p.group) * p.out.head_stride;
-                float* const part = p.few_o + at * D;
-                auto write = [&](uint32_t c, f32x4 x) {     // channels c .. c + 3
-                    if (whole) *reinterpret_cast<u32x2*>(dst + 2 * c) = u32x2{pack2<E>(x[0], x[1]), pack2<E>(x[2], x[3])};
-                    else *reinterpret_cast<f32x4*>(part + c) = x;
-                };
+            auto results = [&](auto write) {                // write(c, x): channels c .. c + 3 of the column's row
                 if constexpr (!kCodes) {
 #pragma unroll
                     for (uint32_t i = 0; i < kOut; ++i) write(16 * i + 4 * quad, o[n][i] * f);
@@ -544,6 +560,46 @@ __global__ __launch_bounds__(kFewThreads, kTiles == 2 && kBits == 16 && D == 128
                         write(32 * b + 8 * quad + 4, f32x4{even[2], odd[2], even[3], odd[3]});
                     }
                 }
+            };
+            auto out_row = [&](uint32_t r) {
+                const uint32_t token = over_group(p, r);
+                return p.out.data + (int64_t)(seq_first + (int32_t)token) * p.out.token_stride + (int64_t)(head * p.group + r - token * p.group) * p.out.head_stride;
+            };
+            if constexpr (kTeam) {
+                __syncthreads();
+                float* const meet = reinterpret_cast<float*>(lds);
+                results([&](uint32_t c, f32x4 x) { *reinterpret_cast<f32x4*>(meet + (wave * 16 + col) * kOutStride + c) = x; });
+                if (quad == 0) lds_m[wave][col] = m[n], lds_l[wave][col] = sum;
+                __syncthreads();
+                constexpr uint32_t kRowThreads = kWaves * kLanes / 16, kPer = D / kRowThreads;   // threads of a row, channels of a thread
+                const uint32_t r = threadIdx.x / kRowThreads, c0 = threadIdx.x % kRowThreads * kPer;
+                if (n * 16 + r < rows) {
+                    float top = -INFINITY, total = 0.0f, acc[kPer];
+#pragma unroll
+                    for (uint32_t v = 0; v < kWaves; ++v) top = fmaxf(top, lds_m[v][r]);
+                    const float from = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+                    for (uint32_t c = 0; c < kPer; ++c) acc[c] = 0.0f;
+#pragma unroll
+                    for (uint32_t v = 0; v < kWaves; ++v) {
+                        const float weight = exp2_of(lds_m[v][r] - from);
+                        total += weight * lds_l[v][r];
+#pragma unroll
+                        for (uint32_t c = 0; c < kPer; ++c) acc[c] += lds_m[v][r] == -INFINITY ? 0.0f : weight * meet[(v * 16 + r) * kOutStride + c0 + c];
+                    }
+                    const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+                    uint32_t* const dst = reinterpret_cast<uint32_t*>(out_row(n * 16 + r) + 2 * c0);
+#pragma unroll
+                    for (uint32_t c = 0; c < kPer; c += 2) dst[c / 2] = pack2<E>(acc[c] * inv, acc[c + 1] * inv);
+                }
+            } else if (row < rows) {
+                const uint64_t at = (uint64_t)slot * p.few_stride + row;
+                char* const dst = out_row(row);
+                float* const part = p.few_o + at * D;
+                results([&](uint32_t c, f32x4 x) {
+                    if (whole) *reinterpret_cast<u32x2*>(dst + 2 * c) = u32x2{pack2<E>(x[0], x[1]), pack2<E>(x[2], x[3])};
+                    else *reinterpret_cast<f32x4*>(part + c) = x;
+                });
                 if (!whole && quad == 0) p.few_ml[at] = f32x2{m[n], sum};
             }
         }

@@ -55,6 +55,38 @@ def test_a_few_new_tokens(new):
     _check(Replica([40, 16, 500, 129], [new] * 4, K=1, A=4))
 
 
+SHARES = [(2, 2, 1), (2, 12, 1), (1, 4, 6), (1, 24, 1)]           # key/value heads, query heads, new tokens: 1, 6 and 24 rows of each head
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("K, A, new", SHARES)
+def test_long_ragged_sequences_dealt_out_evenly(K, A, new, dtype, d, bits):
+    """Sequences that are cut anywhere, some of them longer than what a wavefront takes, one empty."""
+    held = np.array([1, 2100, 0, 40, 700, 33, 1290, 5])
+    _check(Replica(held, np.minimum(held, new), K=K, A=A, d=d, dtype=dtype, bits=bits, page=20))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("K, A, new", [(4, 4, 1), (4, 8, 3), (4, 28, 3)])
+def test_many_short_sequences_uncut(K, A, new, d, bits):
+    held = np.random.default_rng(6).integers(0, 150, 66)
+    _check(Replica(held, np.minimum(held, new), K=K, A=A, d=d, bits=bits, dtype="fp16" if d == 64 else "bf16"))
+    _check(Replica(held, np.minimum(held, new), K=K, A=A, d=d, bits=bits, seed=1), window=30, sinks=2)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_more_sequences_than_a_launch_takes(bits):
+    """Long and short ones beyond the 256 of a launch, beside a prompt."""
+    held = np.random.default_rng(7).integers(0, 40, 600)
+    held[[3, 300, 599]] = 1500, 1300, 200
+    new = np.minimum(held, 1)
+    new[599] = 150
+    _check(Replica(held, new, K=1, A=4, bits=bits))
+
+
 def test_long_axis_is_split_and_joined():
     _check(Replica([5000, 1, 900], [1, 1, 1], K=1, A=8))
     _check(Replica([4000], [70], K=1, A=2, page=64))
