@@ -88,6 +88,9 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
     constexpr uint32_t kLaneRows = kRowBytes / 16;          // lanes that read a row
     constexpr uint32_t kRowsAtOnce = kLanes / kLaneRows, kLoads = kFewKeys / kRowsAtOnce;
     constexpr uint32_t kPairFloats = 2 * kGroups;           // (step, lo) of a key
+    // A maximum is only raised when a score passes it by 2^this; in 4 bits and fp16 that comes off the weights' range.
+    constexpr float kFewHeadroom = kCodes && std::is_same_v<E, fp16> ? 4.0f : 8.0f;
+    constexpr int kWeightExponent = std::is_same_v<E, fp16> ? 10 : 100;
     constexpr uint32_t kWaveBytes = 2 * kSideBytes + (kCodes ? 2 * kFewKeys * kPairFloats * 4 : 0);
     constexpr uint32_t kOutStride = D + 4;                  // floats between rows where a team's results meet
     constexpr uint32_t kJoinBytes = kTeam ? 16 * kOutStride * 4 : 0;
@@ -334,7 +337,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
                     }
                 }
                 if (lane >= kFewKeys) {                 // values: step in the weights' scale, and what the middle code stands for
-                    const float f = power2(kOperandExponent<E> - step_exp);
+                    const float f = power2(kWeightExponent - step_exp);
 #pragma unroll
                     for (uint32_t g = 0; g < kGroups; ++g) par[2 * g + 1] = fmaf(8.0f, par[2 * g], par[2 * g + 1]), par[2 * g] *= f;
                 }
@@ -419,8 +422,9 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
 #pragma unroll
                 for (int j = 1; j < 8; ++j) top = fmaxf(top, x[n][j]);
                 top = max_column(top);
-                if (__any(top > m[n])) {
-                    const float grown = fmaxf(m[n], top), keep = m[n] == -INFINITY ? 0.0f : exp2_of(m[n] - grown);
+                const bool raise = top > m[n] + kFewHeadroom || (m[n] == -INFINITY && top > m[n]);
+                if (__any(raise)) {
+                    const float grown = raise ? top : m[n], keep = raise && m[n] != -INFINITY ? exp2_of(m[n] - grown) : 1.0f;
                     m[n] = grown;
                     l[n] *= keep;
 #pragma unroll
@@ -442,29 +446,33 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
                 }
             }
             if constexpr (kCodes) {
+                auto weigh = [&](auto masked) {
 #pragma unroll
-                for (uint32_t h = 0; h < 2; ++h) {      // keys 4 quad + 0..3 of the first 16, then of the second
-                    float par[4][kPairFloats];
+                    for (uint32_t h = 0; h < 2; ++h) {      // keys 4 quad + 0..3 of the first 16, then of the second
+                        float par[4][kPairFloats];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (uint32_t c = 0; c < kPairFloats; ++c) par[j][c] = v_par[(16 * h + 4 * quad + j) * kPairFloats + c];
+                            for (uint32_t c = 0; c < kPairFloats; ++c) par[j][c] = v_par[(16 * h + 4 * quad + j) * kPairFloats + c];
 #pragma unroll
-                    for (uint32_t n = 0; n < kTiles; ++n)
+                        for (uint32_t n = 0; n < kTiles; ++n)
 #pragma unroll
-                        for (uint32_t g = 0; g < kGroups; ++g) {
-                            float y[4];
+                            for (uint32_t g = 0; g < kGroups; ++g) {
+                                float y[4];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                y[j] = x[n][4 * h + j] * par[j][2 * g];
-                                float low = par[j][2 * g + 1];
-                                if (each && !((shows[n] >> (4 * h + j)) & 1u)) y[j] = 0.0f, low = 0.0f;   // a pair that is NaN reaches nobody who does not see it
-                                lows[n][g] = fmaf(x[n][4 * h + j], low, lows[n][g]);
+                                for (int j = 0; j < 4; ++j) {
+                                    y[j] = x[n][4 * h + j] * par[j][2 * g];
+                                    float low = par[j][2 * g + 1];
+                                    if (masked() && !((shows[n] >> (4 * h + j)) & 1u)) y[j] = 0.0f, low = 0.0f;
+                                    lows[n][g] = fmaf(x[n][4 * h + j], low, lows[n][g]);
+                                }
+                                wg[n][g][2 * h] = pack2<E>(y[0], y[2]);          // keys in spread()'s order: bytes 0 and 2, then 1 and 3
+                                wg[n][g][2 * h + 1] = pack2<E>(y[1], y[3]);
                             }
-                            wg[n][g][2 * h] = pack2<E>(y[0], y[2]);          // keys in spread()'s order: bytes 0 and 2, then 1 and 3
-                            wg[n][g][2 * h + 1] = pack2<E>(y[1], y[3]);
-                        }
-                }
+                    }
+                };
+                if (each) weigh(std::true_type{});          // a pair that is NaN reaches nobody who does not see it
+                else weigh(std::false_type{});
             }
 
             // O^T += V^T P^T: the transposing read gives the lane its 8 keys of one channel (of one byte's two channels)
@@ -541,7 +549,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
             if constexpr (kCodes) {
 #pragma unroll
                 for (uint32_t g = 0; g < kGroups; ++g) low[g] = sum_column(lows[n][g]) * f;
-                f *= power2(kCodeExponent<E> - kOperandExponent<E> + step_exp);
+                f *= power2(kCodeExponent<E> - kWeightExponent + step_exp);
             }
             auto results = [&](auto write) {                // write(c, x): channels c .. c + 3 of the column's row
                 if constexpr (!kCodes) {
