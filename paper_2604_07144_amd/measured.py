@@ -1,0 +1,127 @@
+"""Cost tables with the cache and attention measured on the card.
+
+The roofline prices every operator of a model analytically.  What goes by the lengths in a trace is the cache of keys and
+values and the attention over it; this module runs those (``ap_kv_append``, ``ap_attention``) on the present device at a grid of
+lengths and puts the measured times in the place of the roofline's attention term, so that ``ap_costtable_set`` can score
+candidates with them.  Projections, output head and all-reduce stay the roofline's.
+"""
+from __future__ import annotations
+
+import numpy as np
+import torch
+
+from . import binding
+
+DTYPES = {"bf16": (torch.bfloat16, binding.AP_BF16), "fp16": (torch.float16, binding.AP_FP16)}
+
+
+class ReplicaLayer:
+    """One layer's cache of a replica: ``batch`` slots of up to ``max_len`` tokens in shuffled pages, and a step over them.
+
+    ``heads``, ``kv_heads`` and ``head_dim`` are the layer's; ``bits`` is what the cache is held in (16 or 4).  Caches of
+    ``copies`` layers take turns, as a model's layers do, so that a step does not find its own in the caches of the chip."""
+
+    def __init__(self, batch: int, max_len: int, heads: int, kv_heads: int, head_dim: int, *, dtype: str = "bf16", bits: int = 16,
+                 page: int = 16, copies: int = 1, window: int = 0, sinks: int = 0, device: str = "cuda", seed: int = 0):
+        self.batch, self.max_len, self.heads, self.kv_heads, self.head_dim = batch, max_len, heads, kv_heads, head_dim
+        self.torch_dtype, self.dtype = DTYPES[dtype]
+        self.bits, self.page, self.window, self.sinks, self.device = bits, page, window, sinks, device
+        self.scale = head_dim ** -0.5
+        gen = torch.Generator(device=device)
+        gen.manual_seed(seed)
+        width = -(-max_len // page)
+        self.n_pages = batch * width
+        self.table = torch.randperm(self.n_pages, generator=gen, device=device).int().view(batch, width)
+        row = (self.n_pages, kv_heads, page)
+        self.caches = []
+        for _ in range(copies):
+            if bits == 16:
+                self.caches.append([torch.randn((*row, head_dim), generator=gen, device=device).to(self.torch_dtype) for _ in range(2)])
+            else:
+                codes = [torch.randint(0, 256, (*row, head_dim // 2), generator=gen, device=device, dtype=torch.uint8) for _ in range(2)]
+                pairs = torch.tensor([0.25, -1.875], device=device).to(self.torch_dtype)        # step and lowest value
+                self.caches.append(codes + [pairs.repeat(*row, head_dim // 64, 1).contiguous() for _ in range(2)])
+        angle = torch.arange(max_len, device=device, dtype=torch.float64)[:, None] * \
+            10000.0 ** (-torch.arange(0, head_dim, 2, device=device, dtype=torch.float64) / head_dim)
+        self.turn = torch.stack([angle.cos(), angle.sin()], -1).float()
+        self.gen, self.at = gen, 0
+
+    def plan(self, held: int, new: int) -> dict:
+        """Memory and descriptions of a step in which every slot holds ``held`` tokens, ``new`` of them new."""
+        if not 1 <= new <= held <= self.max_len:
+            raise ValueError(f"a step of {new} new tokens of {held} in slots of {self.max_len}")
+        b, T, made = self.batch, self.batch * new, lambda h: torch.randn((self.batch * new, h, self.head_dim), generator=self.gen, device=self.device).to(self.torch_dtype)
+        p = dict(first=(torch.arange(b + 1, device=self.device) * new).int(), held=torch.full((b,), held, dtype=torch.int32, device=self.device),
+                 q=made(self.heads), k=made(self.kv_heads), v=made(self.kv_heads))
+        p["turned"], p["out"] = torch.empty_like(p["q"]), torch.empty_like(p["q"])
+        p["rows"] = {f: binding.make_rows(p[f].data_ptr(), p[f].shape[1], self.head_dim) for f in ("q", "k", "v", "turned", "out")}
+        p["batch"] = binding.make_seq_batch(b, T, new, held, p["first"].data_ptr(), p["held"].data_ptr(), self.table.data_ptr(), self.table.shape[1])
+        p["caches"] = [binding.make_kv_cache(self.dtype, self.bits, self.n_pages, self.page, self.kv_heads, self.head_dim, *(x.data_ptr() for x in c))
+                       for c in self.caches]
+        p["rotation"] = binding.make_rotation(self.turn.data_ptr(), self.max_len, self.head_dim)
+        p["space"] = torch.empty(max(16, binding.ap_attention_workspace(p["caches"][0], p["batch"], self.heads, self.window, self.sinks)),
+                                 dtype=torch.uint8, device=self.device)
+        return p
+
+    def step(self, p: dict) -> torch.Tensor:
+        """The new tokens into the cache, turned, and their attention over it: [token][head][channel]."""
+        cache, rows, stream = p["caches"][self.at], p["rows"], torch.cuda.current_stream().cuda_stream
+        self.at = (self.at + 1) % len(self.caches)
+        binding.ap_kv_append(cache, p["batch"], rows["k"], rows["v"], p["rotation"], rows["q"], rows["turned"], self.heads, stream)
+        binding.ap_attention(cache, p["batch"], rows["turned"], rows["out"], self.heads, self.scale, self.window, self.sinks,
+                             p["space"].data_ptr(), p["space"].numel(), stream)
+        return p["out"]
+
+    def time_us(self, held: int, new: int, repeats: int = 20) -> float:
+        """Microseconds of a step among others: the median of five timings of ``repeats`` steps each."""
+        p = self.plan(held, new)
+        for _ in range(3):
+            self.step(p)
+        times = []
+        for _ in range(5):
+            a, z = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(repeats):
+                self.step(p)
+            z.record()
+            z.synchronize()
+            times.append(a.elapsed_time(z) * 1e3 / repeats)
+        return float(np.median(times))
+
+
+def layer_times(model, batch: int, contexts, prompts, *, dtype: str = "bf16", bits: int = 16, page: int = 16, window: int = 0,
+                sinks: int = 0, repeats: int = 20):
+    """Measured microseconds of a layer's append and attention: decode steps of ``batch`` sequences at each of ``contexts``,
+    prefills of ``batch`` prompts of each of ``prompts``.  ``model`` is a record of ``binding.MODEL_DTYPE``."""
+    heads, kv_heads, d = int(model["heads"]), int(model["kv_heads"]), int(model["hidden"]) // int(model["heads"])
+    longest = max(*contexts, *prompts)
+    size = 2 * batch * (-(-longest // page) * page) * kv_heads * (2 * d if bits == 16 else d // 2 + d // 16)
+    layer = ReplicaLayer(batch, longest, heads, kv_heads, d, dtype=dtype, bits=bits, page=page, window=window, sinks=sinks,
+                         copies=max(1, min(int(model["layers"]), (1 << 30) // size)))
+    return (np.array([layer.time_us(int(c), 1, repeats) for c in contexts]),
+            np.array([layer.time_us(int(s), int(s), max(2, repeats // 4)) for s in prompts]))
+
+
+def _roofline_attention_us(model, gpu, batch, n, c):
+    """The roofline's time of one layer's attention: n new tokens a sequence over c tokens."""
+    A, K, d, e = float(model["heads"]), float(model["kv_heads"]), float(model["hidden"]) / float(model["heads"]), float(model["weight_bits"]) / 8.0
+    flops, nbytes = 4.0 * batch * n * c * A * d, e * (2.0 * batch * n * A * d + 2.0 * batch * c * K * d)
+    return flops / np.minimum(flops / nbytes * gpu["hbm_bytes_per_s"], gpu["flops"]) * 1e6
+
+
+def request_tables(model, gpu, batch: int, prompt_len, out_len, contexts, decode_us, prompts, prefill_us):
+    """``prefill_us`` and ``tpot_us`` (uint32 [1][R], for ``ap_costtable_set``) of requests on a replica of one GPU: the roofline's
+    times with its attention term replaced by the measured ones, which are interpolated between the lengths they were taken at."""
+    prompt, out = np.asarray(prompt_len, np.int64), np.asarray(out_len, np.int64)
+    longest = int((prompt + out).max())
+    group = np.array([(0, 0, 1, batch)], dtype=binding.GROUP_DTYPE)
+    pre_ns, prefix_ns, _, _ = binding.ap_roofline_tables(np.array([model], binding.MODEL_DTYPE), np.array([gpu], binding.GPU_DTYPE), group, longest)
+    length = np.arange(1, longest + 1, dtype=np.float64)
+    layers = float(model["layers"])
+    change = lambda grid, us, n: layers * (np.interp(length, grid, us) - _roofline_attention_us(model, gpu, batch, n, length))   # noqa: E731
+    pre = np.asarray(pre_ns, np.float64).reshape(-1)[1:longest + 1] / 1e3 + change(prompts, prefill_us, length)
+    step = np.diff(np.asarray(prefix_ns, np.float64).reshape(-1))[1:longest + 1] / 1e3 + change(contexts, decode_us, 1.0)
+    upto = np.concatenate([[0.0], np.cumsum(step)])          # of contexts 1 .. k
+    tpot = (upto[prompt + out - 1] - upto[prompt - 1]) / out
+    whole = lambda x: np.maximum(1, np.rint(x)).astype(np.uint32)[None]   # noqa: E731
+    return whole(pre[prompt - 1]), whole(tpot)
