@@ -39,13 +39,11 @@ __device__ __forceinline__ u32x2 lds_transposed8(const char* at) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((Ptr)(at)));
 }
 
-// A power of two with the exponent e.
-__device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
-// The exponent above x > 0: x < 2^e.
-__device__ __forceinline__ int exponent_above(float x) { return (int)(__float_as_uint(x) >> 23) - 126; }
-
 template <typename E> constexpr int kCodeExponent = std::is_same_v<E, bf16> ? 133 : 24;      // a code n as bits: n * 2^-this
 template <typename E> constexpr int kOperandExponent = std::is_same_v<E, bf16> ? 100 : 14;   // the other operand is brought below 2^this
+// Steps of values from here on stay out of the products, so that no such step, which perhaps few rows see, takes the others'
+// weights out of the operand's range.
+template <typename E> constexpr float kStepMost = std::is_same_v<E, bf16> ? 65536.0f : 8.0f;
 
 // 16 codes of 8 bytes' halves as two operands: per dword bytes 0 and 2, low and high halves (times 16), then bytes 1 and 3
 __device__ __forceinline__ u32x4 spread(uint32_t x) {
@@ -297,6 +295,8 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
 
         for (uint32_t tile = first_tile; tile < last_tile; tile += kStep) {
             const uint32_t seen = seen_next;
+            uint32_t apart = 0;                         // one bit a key: one of its values' steps is above kStepMost
+            float apart_step[kGroups];                  // lanes from 32 on: these steps, others 0
             // rows to LDS; values (in 4 bits: pairs) that are not there as zeros
             if (!kCodes && seen != ~0u) {
 #pragma unroll
@@ -316,13 +316,19 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
 #pragma unroll
                 for (uint32_t g = 0; g < kGroups; ++g) {
                     par[2 * g] = there ? low16<E>(raw_pair[g]) : 0.0f, par[2 * g + 1] = there ? high16<E>(raw_pair[g]) : 0.0f;
-                    larger |= lane >= kFewKeys && fabsf(par[2 * g]) < INFINITY && fabsf(par[2 * g]) >= power2(step_exp);
+                    const float step = fabsf(par[2 * g]);
+                    const bool out = lane >= kFewKeys && step < INFINITY && step >= kStepMost<E>;
+                    apart_step[g] = out ? par[2 * g] : 0.0f;
+                    larger |= lane >= kFewKeys && step < kStepMost<E> && step >= power2(step_exp);
                 }
+                bool out = apart_step[0] != 0.0f;
+                if constexpr (kGroups == 2) out |= apart_step[kGroups - 1] != 0.0f;
+                apart = (uint32_t)(__ballot(out) >> kFewKeys);
                 if (__any(larger)) {                    // a larger step than any so far (the first steps do this, seldom others)
                     float most = 0.0f;
 #pragma unroll
                     for (uint32_t g = 0; g < kGroups; ++g)
-                        if (lane >= kFewKeys && fabsf(par[2 * g]) < INFINITY) most = fmaxf(most, fabsf(par[2 * g]));
+                        if (lane >= kFewKeys && fabsf(par[2 * g]) < kStepMost<E>) most = fmaxf(most, fabsf(par[2 * g]));
 #pragma unroll
                     for (uint32_t x = 1; x < kLanes; x *= 2) most = fmaxf(most, __shfl_xor(most, x));
                     const int e = __builtin_amdgcn_readfirstlane(exponent_above(most));
@@ -339,7 +345,10 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
                 if (lane >= kFewKeys) {                 // values: step in the weights' scale, and what the middle code stands for
                     const float f = power2(kWeightExponent - step_exp);
 #pragma unroll
-                    for (uint32_t g = 0; g < kGroups; ++g) par[2 * g + 1] = fmaf(8.0f, par[2 * g], par[2 * g + 1]), par[2 * g] *= f;
+                    for (uint32_t g = 0; g < kGroups; ++g) {
+                        if (apart_step[g] != 0.0f) par[2 * g] = 0.0f;
+                        par[2 * g + 1] = fmaf(8.0f, par[2 * g], par[2 * g + 1]), par[2 * g] *= f;
+                    }
                 }
                 float* to = (lane < kFewKeys ? k_par : v_par) + (lane % kFewKeys) * kPairFloats;
                 if constexpr (kGroups == 2) *reinterpret_cast<f32x4*>(to) = f32x4{par[0], par[1], par[2], par[3]};
@@ -471,6 +480,27 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
                             }
                     }
                 };
+                for (uint32_t left = apart; left; left &= left - 1) {       // key by key, in 32 bits
+                    const uint32_t k = (uint32_t)__builtin_ctz(left), j = (k / 16) * 4 + k % 4;
+                    const float scale = power2(kWeightExponent - kCodeExponent<E> - step_exp);
+#pragma unroll
+                    for (uint32_t n = 0; n < kTiles; ++n) {
+                        float weight = x[n][0];
+#pragma unroll
+                        for (uint32_t i = 1; i < 8; ++i) weight = i == j ? x[n][i] : weight;
+                        weight = __shfl(weight, (int)(k % 16 / 4 * 16 + col));
+#pragma unroll
+                        for (uint32_t b = 0; b < kOut / 2; ++b) {
+                            const float step = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(apart_step[b / 2]), kFewKeys + k)) * scale * weight;
+                            const uint32_t codes = *reinterpret_cast<const uint32_t*>(v_lds + v_at(k, b) + 4 * quad);
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                o[n][2 * b][c] += step * (float)(codes >> (8 * c) & 15u);
+                                o[n][2 * b + 1][c] += step * (float)(codes >> (8 * c) & 0xF0u);
+                            }
+                        }
+                    }
+                }
                 if (each) weigh(std::true_type{});          // a pair that is NaN reaches nobody who does not see it
                 else weigh(std::false_type{});
             }

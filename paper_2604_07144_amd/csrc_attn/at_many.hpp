@@ -18,6 +18,34 @@
 namespace {
 
 constexpr float kHeadroom = 8.0f;
+// Weights in fp16 are held times 2^this: with the headroom their largest is 2^15, and none above 2^-31 of the maximum is lost.
+template <typename P> constexpr float kWeightUp = std::is_same_v<P, fp16> ? 7.0f : 0.0f;
+
+// A cache in 4 bits is decoded to fp16, whose 11 bits keep codes of 4 on a lowest value and step of 8 where bf16 would round
+// them away (error of a chunk's results 0.0039 -> REL, against 0.0017 of the final rounding alone).  With bf16 pairs that
+// holds a tile whose groups all lie, by their largest magnitude, from 2^-5 up to 2^14 (keys) and 2^8 (values), or are zero:
+// what fp16 then loses is below 2^-20 of the group.  Any other tile is decoded to bf16 and multiplied as that.
+constexpr float kGroupLeast = 0.03125f, kKeyMost = 16384.0f, kValueMost = 256.0f;
+template <typename E> __device__ __forceinline__ bool ordinary(uint32_t key_pair, uint32_t value_pair) {
+    auto most = [](uint32_t pr) { return fmaxf(fabsf(high16<E>(pr)), fabsf(fmaf(15.0f, low16<E>(pr), high16<E>(pr)))) + 0.0f * low16<E>(pr); };
+    const float k = most(key_pair), v = most(value_pair);
+    if constexpr (std::is_same_v<E, fp16>) return v < 65504.0f;              // decoded alike; the values are finite
+    else return ((k >= kGroupLeast && k < kKeyMost) || k == 0.0f) && ((v >= kGroupLeast && v < kValueMost) || v == 0.0f);
+}
+
+// Eight codes of a dword as fp16: 1024 + code, whose bits are the code's beside an exponent, gives the code exactly, and one
+// multiply-add the value, rounded once.  `pair` is (step, lo) in fp16.
+__device__ __forceinline__ u32x4 decode8_fp16(uint32_t codes, Vec2<fp16> pair) {
+    const Vec2<fp16> unit = {(fp16)1.0f, (fp16)0.0625f}, bias = {(fp16)-1024.0f, (fp16)-64.0f}, step = {pair[0], pair[0]}, lo = {pair[1], pair[1]};
+    u32x4 r;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {                      // a byte's low code in the low half, its high code, times 16, in the high half
+        const uint32_t x = __builtin_amdgcn_perm(0x64646464u, codes, 0x04000400u + i * 0x00010001u) & 0x64F0640Fu;
+        r[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_elementwise_fma(__builtin_bit_cast(Vec2<fp16>, x), unit, bias), step, lo));
+    }
+    return r;
+}
+template <typename E> __device__ __forceinline__ Vec2<fp16> pair_fp16(uint32_t pr) { return Vec2<fp16>{(fp16)low16<E>(pr), (fp16)high16<E>(pr)}; }
 
 __device__ const u32x4 kZeroRow[16] = {};                   // stands in for keys and values that are not there
 
@@ -58,9 +86,13 @@ template <uint32_t D> __device__ __forceinline__ uint32_t value_piece(uint32_t k
 template <typename E, uint32_t D, uint32_t kBits>
 __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) void k_attend_many(const AttnParams p, const uint32_t n_row_tiles, const uint32_t n_chunks) {
     constexpr uint32_t kSteps = D / 16, kOut = D / 32, kPieces = D / 8;
+    constexpr bool kCodes = kBits == 4;
+    using P = std::conditional_t<kCodes, fp16, E>;          // what ordinary tiles are multiplied in
+    constexpr bool kMixed = !std::is_same_v<P, E>;
     __shared__ u32x4 lds_k[2][kManyKeys * kPieces], lds_v[2][kManyKeys * kPieces];
     __shared__ const char *lds_at_k[2][kManyKeys], *lds_at_v[2][kManyKeys];                // where the rows of a tile lie
-    __shared__ int64_t lds_pairs[kBits == 4 ? 2 : 1][kManyKeys];
+    __shared__ u32x4 lds_pairs[kCodes ? 2 : 1][kManyKeys];  // of a key's groups, then of a value's
+    __shared__ uint32_t lds_odd[4];                         // as lds_seen: a key is not ordinary()
     __shared__ uint32_t lds_strange;                        // the last tile, counted from 1, whose values hold a NaN or an infinity
     __shared__ uint64_t lds_seen[4];                        // one bit a key: it is there; written two tiles ahead, while the present one's is read
 
@@ -88,11 +120,27 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
     const int32_t pos_first = seq.pos0 + (int32_t)over_group(p, min(row0 + wave * 32, rows - 1));
     const int32_t pos_last = seq.pos0 + (int32_t)over_group(p, min(row0 + wave * 32 + 31, rows - 1));
 
+    const char* const q_row = p.q.data + (int64_t)(seq.first + (int32_t)token) * p.q.token_stride + (int64_t)(head * p.group + r - token * p.group) * p.q.head_stride + 16 * half;
     u32x4 q[kSteps];
-    {
-        const char* row = p.q.data + (int64_t)(seq.first + (int32_t)token) * p.q.token_stride + (int64_t)(head * p.group + r - token * p.group) * p.q.head_stride;
 #pragma unroll
-        for (uint32_t i = 0; i < kSteps; ++i) q[i] = *reinterpret_cast<const u32x4*>(row + 32 * i + 16 * half);
+    for (uint32_t i = 0; i < kSteps; ++i) q[i] = *reinterpret_cast<const u32x4*>(q_row + 32 * i);
+    float q_unit = p.scale_log2;                            // of the scores, in powers of two
+    if constexpr (kMixed) {                                 // to fp16: the row's largest is brought just below 2^14 by a power of two
+        float most = 0.0f;
+#pragma unroll
+        for (uint32_t i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float a = fabsf(low16<E>(q[i][j])), b = fabsf(high16<E>(q[i][j]));
+                most = fmaxf(most, fmaxf(a < INFINITY ? a : 0.0f, b < INFINITY ? b : 0.0f));
+            }
+        const int e = max(exponent_above(max_halves(most)), -100);
+        const float up = power2(14 - e);
+        q_unit *= power2(e - 14);
+#pragma unroll
+        for (uint32_t i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[i][j] = pack2<P>(low16<E>(q[i][j]) * up, high16<E>(q[i][j]) * up);
     }
     f32x16 o[kOut];
 #pragma unroll
@@ -104,8 +152,21 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
     const int32_t* table = p.batch.table + (int64_t)s * p.batch.table_stride;
     const int64_t head_at = (int64_t)head * p.cache.head_stride, pair_head_at = (int64_t)head * p.cache.pair_head_stride;
 
-    // ---- where a tile's keys lie: one wavefront looks them up, a lane a key, two tiles ahead
+    // ---- where a tile's keys lie: one wavefront looks them up, a lane a key, two tiles ahead; in 4 bits three, and reads their
+    // pairs one tile later
     Place ahead;
+    u32x4 ahead_pairs = {0, 0, 0, 0};
+    auto fetch_pairs = [&]() {
+        ahead_pairs = u32x4{0, 0, 0, 0};
+        if (!ahead.there) return;
+        const int64_t at = ahead.page * p.cache.pair_page_stride + ahead.slot * p.cache.pair_slot_stride + pair_head_at;
+        if constexpr (D == 128) {
+            const u32x2 k = *reinterpret_cast<const u32x2*>(p.cache.k_pairs + at), v = *reinterpret_cast<const u32x2*>(p.cache.v_pairs + at);
+            ahead_pairs = u32x4{k[0], k[1], v[0], v[1]};
+        } else {
+            ahead_pairs[0] = *reinterpret_cast<const uint32_t*>(p.cache.k_pairs + at), ahead_pairs[2] = *reinterpret_cast<const uint32_t*>(p.cache.v_pairs + at);
+        }
+    };
     auto places = [&](uint32_t tile) {
         int32_t base, end;
         tile_at<kManyKeys>(sp, tile, base, end);
@@ -118,7 +179,11 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
         const char* zero = kBits == 16 ? reinterpret_cast<const char*>(kZeroRow) : nullptr;
         lds_at_k[buf][lane] = ahead.there ? p.cache.k + row : zero;
         lds_at_v[buf][lane] = ahead.there ? p.cache.v + row : zero;
-        if constexpr (kBits == 4) lds_pairs[buf][lane] = ahead.page * p.cache.pair_page_stride + ahead.slot * p.cache.pair_slot_stride + pair_head_at;
+        if constexpr (kCodes) {
+            lds_pairs[buf][lane] = ahead_pairs;
+            const bool odd = __any(!ordinary<E>(ahead_pairs[0], ahead_pairs[2]) || (D == 128 && !ordinary<E>(ahead_pairs[1], ahead_pairs[3])));
+            if (lane == 0) lds_odd[tile & 3u] = odd;
+        }
         if (lane == 0) lds_seen[tile & 3u] = seen;
     };
 
@@ -127,7 +192,6 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
     constexpr uint32_t kRows = kLanes / kPieces, kLoads = kManyKeys / kRows / kManyWaves;
     constexpr uint32_t kCodePieces = D / 32, kCodeThreads = kManyKeys * kCodePieces;
     u32x4 raw_k = {0, 0, 0, 0}, raw_v = {0, 0, 0, 0};
-    uint32_t pair_k = 0, pair_v = 0;
     const uint32_t code_key = threadIdx.x / kCodePieces, code_piece = threadIdx.x % kCodePieces;
     auto fetch = [&](uint32_t buf) {
         if constexpr (kBits == 16) {
@@ -139,23 +203,32 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
             }
         } else if (kCodeThreads >= kManyThreads || threadIdx.x < kCodeThreads) {
             const char *at_k = lds_at_k[buf][code_key], *at_v = lds_at_v[buf][code_key];
-            const int64_t pr = lds_pairs[buf][code_key] + 4 * (code_piece / 2);
-            raw_k = raw_v = u32x4{0, 0, 0, 0}, pair_k = pair_v = 0;
+            raw_k = raw_v = u32x4{0, 0, 0, 0};
             if (at_k) {
                 raw_k = *reinterpret_cast<const u32x4*>(at_k + 16 * code_piece);
                 raw_v = *reinterpret_cast<const u32x4*>(at_v + 16 * code_piece);
-                pair_k = *reinterpret_cast<const uint32_t*>(p.cache.k_pairs + pr);
-                pair_v = *reinterpret_cast<const uint32_t*>(p.cache.v_pairs + pr);
             }
         }
     };
-    auto put = [&](uint32_t buf) {
-        if constexpr (kBits == 4) {
+    auto put = [&](uint32_t tile) {                         // counted from the first
+        if constexpr (kCodes) {
             if (kCodeThreads >= kManyThreads || threadIdx.x < kCodeThreads) {
+                const uint32_t buf = tile & 1u;
+                const uint32_t* const pairs = reinterpret_cast<const uint32_t*>(&lds_pairs[buf][code_key]) + code_piece / 2;
+                const uint32_t pair_k = pairs[0], pair_v = pairs[2];
+                if (!kMixed || !uniform(lds_odd[tile & 3u])) {
+                    const Vec2<fp16> half_k = pair_fp16<E>(pair_k), half_v = pair_fp16<E>(pair_v);
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    lds_k[buf][code_key * kPieces + key_piece<D>(code_key, 4 * code_piece + i)] = decode8<E>(raw_k[i], low16<E>(pair_k), high16<E>(pair_k));
-                    lds_v[buf][code_key * kPieces + value_piece<D>(code_key, 4 * code_piece + i)] = decode8<E>(raw_v[i], low16<E>(pair_v), high16<E>(pair_v));
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        lds_k[buf][code_key * kPieces + key_piece<D>(code_key, 4 * code_piece + i)] = decode8_fp16(raw_k[i], half_k);
+                        lds_v[buf][code_key * kPieces + value_piece<D>(code_key, 4 * code_piece + i)] = decode8_fp16(raw_v[i], half_v);
+                    }
+                } else {
+#pragma unroll 1
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        lds_k[buf][code_key * kPieces + key_piece<D>(code_key, 4 * code_piece + i)] = decode8<E>(raw_k[i], low16<E>(pair_k), high16<E>(pair_k));
+                        lds_v[buf][code_key * kPieces + value_piece<D>(code_key, 4 * code_piece + i)] = decode8<E>(raw_v[i], low16<E>(pair_v), high16<E>(pair_v));
+                    }
                 }
             }
         }
@@ -165,10 +238,17 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
     const int32_t all_first = seq.pos0 + (int32_t)uniform(over_group(p, row0)), all_last = seq.pos0 + (int32_t)uniform(over_group(p, row1));
 
     if (threadIdx.x == 0) lds_strange = 0;
-    if (wave == 0) places(first_tile), put_places(0);
+    auto begin_with = [&](uint32_t tile) {                  // counted from the first
+        places(first_tile + tile);
+        if constexpr (kCodes) fetch_pairs();
+        put_places(tile);
+    };
+    constexpr uint32_t kLookAhead = kCodes ? 3 : 2;
+    if (wave == 0) begin_with(0);
     __syncthreads();
     fetch(0);
-    if (wave == 0) places(first_tile + 1), put_places(1);
+    if (wave == 0) begin_with(1);
+    if (kCodes && wave == kManyWaves - 1) places(first_tile + 2);
     put(0);
     wait_loads();
     __syncthreads();
@@ -176,15 +256,18 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
         const uint32_t buf = (tile - first_tile) & 1u;
         const uint64_t seen_all = lds_seen[(tile - first_tile) & 3u];
         const uint32_t seen_lo = __builtin_amdgcn_readfirstlane((uint32_t)seen_all), seen_hi = __builtin_amdgcn_readfirstlane((uint32_t)(seen_all >> 32));
+        const uint32_t odd = kCodes ? uniform(lds_odd[(tile - first_tile) & 3u]) : 1u;
         if (tile + 1 < last_tile) fetch(buf ^ 1u);
-        const bool mine = (tile & (kManyWaves - 1)) == wave;
-        if (mine) places(tile + 2);
+        const uint32_t turn = tile - first_tile;
+        const bool puts = ((turn + kManyWaves - (kLookAhead - 2)) & (kManyWaves - 1)) == wave;
+        if (kCodes && puts) fetch_pairs();
+        if ((turn & (kManyWaves - 1)) == wave) places(tile + kLookAhead);
         int32_t base, end;
         tile_at<kManyKeys>(sp, tile, base, end);
         const bool sink_part = tile < sp.sink_tiles;
         // Where not all rows see all keys, a NaN or infinity among the values must not reach the others as 0 * NaN: the rows
         // that see it take it as it is (a weight does not change it), and zero stands in for it.
-        if (base + (int32_t)kManyKeys - 1 > all_first || (p.window && !sink_part && (int64_t)base <= (int64_t)all_last - p.window)) {
+        if (odd && (base + (int32_t)kManyKeys - 1 > all_first || (p.window && !sink_part && (int64_t)base <= (int64_t)all_last - p.window))) {
             constexpr uint32_t kMine = kManyKeys * kPieces / kManyThreads;
             uint32_t bad = 0;                               // the exponent, all ones, carries into the sign's place
 #pragma unroll
@@ -225,7 +308,15 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
             }
         }
         // work, unless all of the tile lies after the wavefront's rows or before their windows
-        if (base <= pos_last && !(p.window && !sink_part && (uint32_t)base >= p.sinks && (int64_t)base + kManyKeys - 1 <= (int64_t)pos_first - p.window)) {
+        auto work = [&](auto type) {
+            using T = decltype(type);
+            constexpr bool kGiven = !std::is_same_v<T, P>;  // queries as they were given, from memory: seldom needed, no registers
+            const float unit = kGiven ? p.scale_log2 : q_unit;
+            auto query = [&](uint32_t i) {
+                if constexpr (!kGiven) return q[i];
+                asm volatile("" : : : "memory");
+                return *reinterpret_cast<const u32x4*>(q_row + 32 * i);
+            };
             const char* const keys = reinterpret_cast<const char*>(lds_k[buf]);
             const char* const values = reinterpret_cast<const char*>(lds_v[buf]);
             f32x16 sc[2];
@@ -236,10 +327,12 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
             // pieces are told apart by exclusive or, so one number and the product's give the place
             const uint32_t key_at = here(col * (2 * D) + key_piece<D>(col, half) * 16);
 #pragma unroll
-            for (uint32_t i = 0; i < kSteps; ++i)
+            for (uint32_t i = 0; i < kSteps; ++i) {
+                const u32x4 x = query(i);
 #pragma unroll
                 for (uint32_t t = 0; t < 2; ++t)
-                    sc[t] = mfma32<E>(*reinterpret_cast<const u32x4*>(keys + 32 * t * (2 * D) + (key_at ^ (32 * i))), q[i], sc[t]);
+                    sc[t] = mfma32<T>(*reinterpret_cast<const u32x4*>(keys + 32 * t * (2 * D) + (key_at ^ (32 * i))), x, sc[t]);
+            }
             // six operands are read ahead of the products
             __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
@@ -271,7 +364,7 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
             float top = sc[0][0];
 #pragma unroll
             for (int j = 1; j < 32; ++j) top = fmaxf(top, sc[j / 16][j % 16]);
-            top = max_halves(top) * p.scale_log2;
+            top = max_halves(top) * unit;
             const bool raise = top > m + kHeadroom || (m == -INFINITY && top > m);
             if (__any(raise)) {
                 const float grown = raise ? top : m, keep = raise && m != -INFINITY ? exp2_of(m - grown) : 1.0f;
@@ -282,15 +375,15 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
 #pragma unroll
                     for (int j = 0; j < 16; ++j) o[i][j] *= keep;
             }
-            const float from = m == -INFINITY ? 0.0f : m;
+            const float from = m == -INFINITY ? 0.0f : m - kWeightUp<P>;
             u32x4 w[4];                                     // weights of 16 keys each, as the second product takes them
 #pragma unroll
             for (uint32_t t = 0; t < 2; ++t)
 #pragma unroll
                 for (int j = 0; j < 16; j += 2) {
-                    const float a = exp2_of(fmaf(sc[t][j], p.scale_log2, -from)), b = exp2_of(fmaf(sc[t][j + 1], p.scale_log2, -from));
+                    const float a = exp2_of(fmaf(sc[t][j], unit, -from)), b = exp2_of(fmaf(sc[t][j + 1], unit, -from));
                     l += a + b;
-                    w[2 * t + j / 8][j % 8 / 2] = pack2<E>(a, b);
+                    w[2 * t + j / 8][j % 8 / 2] = pack2<T>(a, b);
                 }
             const uint32_t key_in = 4 * half + (lane % 16) / 4, piece_in = ((lane / 16) % 2) * 2 + (lane % 4) / 2, byte_in = (lane % 2) * 8;
             const uint32_t value_at = here(key_in * (2 * D) + value_piece<D>(key_in, piece_in) * 16 + byte_in);
@@ -300,11 +393,19 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
                 for (uint32_t i = 0; i < kOut; ++i) {
                     const char* at = values + (value_at ^ (64 * i));
                     const u32x2 lo = lds_transposed(at + 16 * t * (2 * D)), hi = lds_transposed(at + (16 * t + 8) * (2 * D));
-                    o[i] = mfma32<E>(u32x4{lo[0], lo[1], hi[0], hi[1]}, w[t], o[i]);
+                    o[i] = mfma32<T>(u32x4{lo[0], lo[1], hi[0], hi[1]}, w[t], o[i]);
                 }
+        };
+        if (base <= pos_last && !(p.window && !sink_part && (uint32_t)base >= p.sinks && (int64_t)base + kManyKeys - 1 <= (int64_t)pos_first - p.window)) {
+            if constexpr (kMixed) {
+                if (odd) work(E{});
+                else work(P{});
+            } else {
+                work(P{});
+            }
         }
-        if (tile + 1 < last_tile) put(buf ^ 1u);
-        if (mine) put_places(tile - first_tile + 2);
+        if (tile + 1 < last_tile) put(turn + 1);
+        if (puts) put_places(turn + 2);
         wait_loads();
         __syncthreads();
     }
@@ -332,7 +433,7 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
                 const f32x4 x = {o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]};
                 *reinterpret_cast<f32x4*>(p.many_o + at * D + 32 * i + 2 * j + 4 * half) = x;
             }
-        if (half == 0) p.many_ml[at] = f32x2{m, total};
+        if (half == 0) p.many_ml[at] = f32x2{m - kWeightUp<P>, total};
     }
 }
 

@@ -77,6 +77,11 @@ __device__ __forceinline__ bool not_finite16(uint32_t two, uint32_t exponent) {
 template <typename E> constexpr uint32_t kExponentStep = std::is_same_v<E, bf16> ? 0x00800080u : 0x04000400u;   // 1 in both exponents of a dword
 template <typename E> constexpr uint32_t kExponent = std::is_same_v<E, bf16> ? 0x7F80u : 0x7C00u;
 
+// A power of two with the exponent e.
+__device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// The exponent above x > 0: x < 2^e.
+__device__ __forceinline__ int exponent_above(float x) { return (int)(__float_as_uint(x) >> 23) - 126; }
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126: 0
 
 // Joins the parts of a row, which lie at `at(0)` .. `at(n - 1)`.  Each lane has the (m, l) of a part; then 16 lanes read the
