@@ -88,7 +88,17 @@ struct Plan {
     uint64_t plan_bytes, bytes;
 };
 
-constexpr uint32_t kResident = 512;      // workgroups that the chip holds of the kernels: two on each of 256 CUs (one where rows need all registers)
+constexpr uint32_t kCus = 256, kResident = 2 * kCus;   // workgroups that the chip holds of the kernel of many rows: two on each CU
+
+// Workgroups on a CU of the kernel of few rows on the line, which a wavefront's share of it has to be worth: with 64 channels in
+// 4 bits four on a SIMD against two take 0.84 to 0.94 of the time where each has 12 to 24 places, 0.99 to 1.02 with 3.4 to 6,
+// and 1.17 with 3.  (16 bits with 64 channels, and 4 bits with 128, lose 1.03 to 1.25 by a third one.)
+constexpr uint32_t kPlacesOfFour = 8;
+uint32_t per_cu(uint32_t d, uint32_t bits, uint32_t tiles, uint64_t units) {
+    uint32_t n = 0;
+    for_dim(d, [&](auto dim) { for_bits(bits, [&](auto b) { n = tiles == 1 ? kFewPerSimd<dim(), b(), 1, false> : kFewPerSimd<dim(), b(), 2, false>; }); });
+    return n == 4 && units < (uint64_t)kPlacesOfFour * 4 * kCus * kLineWaves ? 2 : n;
+}
 
 // How the kernel of few rows deals out its work.  32 heads on 8, 128 channels, bf16, sequences of one length, us:
 //  - A team for each (sequence, head) while these are fewer than the chip's 256 CUs, and not so long that a ragged batch,
@@ -125,7 +135,7 @@ ap_status plan_of(const ap_kv_cache* c, const Batch& b, uint32_t q_heads, uint32
         } else if (tiles <= (pairs >= kManyPairs ? kUncutTilesOfMany : kUncutTiles)) {
             r.few_groups = (uint32_t)((pairs + kLineWaves - 1) / kLineWaves);
         } else {
-            r.few_groups = (uint32_t)std::min<uint64_t>((units + kLineWaves - 1) / kLineWaves, r.few_tiles == 2 && c->head_dim == 128 ? kResident / 2 : kResident);
+            r.few_groups = (uint32_t)std::min<uint64_t>((units + kLineWaves - 1) / kLineWaves, kCus * per_cu(c->head_dim, c->bits, r.few_tiles, units));
             r.plan_bytes = (4ull * (r.few_seqs + 2) + 15) / 16 * 16;
             r.few_n = 2ull * r.few_groups * kLineWaves * r.few_stride;
         }

@@ -75,9 +75,13 @@ struct FewSeq {
 template <uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
 constexpr uint32_t kFewWaves = kTeam && !(D == 128 && kBits == 16 && kTiles == 2) ? 8 : 4;
 
+// Wavefronts that registers leave room for on a SIMD.
+template <uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
+constexpr uint32_t kFewPerSimd = kTiles == 2 && D == 128 && (kBits == 16 || !kTeam) ? 1 : kTiles == 1 && D == 64 && kBits == 4 && !kTeam ? 4 : 2;
+
 // kTiles: tiles of 16 rows.  kTeam: a workgroup takes a (sequence, head) and joins its wavefronts' parts itself.
 template <typename E, uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
-__global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTiles == 2 && D == 128 && (kBits == 16 || !kTeam) ? 1 : 2)) void k_attend_few(const AttnParams p) {
+__global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFewPerSimd<D, kBits, kTiles, kTeam>)) void k_attend_few(const AttnParams p) {
     constexpr uint32_t kWaves = kFewWaves<D, kBits, kTiles, kTeam>;
     constexpr bool kCodes = kBits == 4;
     constexpr uint32_t kGroups = D / 64;
@@ -203,35 +207,38 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
         const int32_t* table = p.batch.table + (int64_t)s * p.batch.table_stride;
         const int64_t head_at = (int64_t)head * p.cache.head_stride, pair_head_at = (int64_t)head * p.cache.pair_head_stride;
         Place ahead;
-        u32x4 raw_k[kLoads], raw_v[kLoads];
-        u32x2 raw_pair;                             // of the keys (lanes below 32) or the values
-        uint32_t seen_next;                         // one bit a key of the tile: it is there
+        struct {
+            u32x4 k[kLoads], v[kLoads];
+            u32x2 pair;                             // of the keys (lanes below 32) or the values
+            uint32_t seen;                          // one bit a key of the tile: it is there
+        } raw;
         auto places = [&](uint32_t tile) {
             int32_t base, end;
             tile_at<kFewKeys>(sp, tile, base, end);
             ahead = place_of(p.cache, table, tile < last_tile ? (uint32_t)(base + (int32_t)(lane % kFewKeys)) : 0xFFFFFFFFu, (uint32_t)end);
         };
-        auto fetch = [&]() {                                // where nothing is, the cache's first row stands in
-            seen_next = (uint32_t)__ballot(ahead.there);
+        // The places of the tile after are asked for before the rows, so that waiting for them does not wait for the rows too.
+        auto fetch = [&](uint32_t next) {         // where nothing is, the cache's first row stands in
+            raw.seen = (uint32_t)__ballot(ahead.there);
             const int64_t page = ahead.there ? ahead.page : 0, slot = ahead.there ? ahead.slot : 0;
             if (lane < kFewKeys) lds_rows[wave][lane] = page * p.cache.page_stride + slot * p.cache.slot_stride + head_at;
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            places(next);
 #pragma unroll
             for (uint32_t i = 0; i < kLoads; ++i) {
                 const int64_t at = lds_rows[wave][i * kRowsAtOnce + load_row] + 16 * load_piece;
-                raw_k[i] = *reinterpret_cast<const u32x4*>(p.cache.k + at);
-                raw_v[i] = *reinterpret_cast<const u32x4*>(p.cache.v + at);
+                raw.k[i] = *reinterpret_cast<const u32x4*>(p.cache.k + at);
+                raw.v[i] = *reinterpret_cast<const u32x4*>(p.cache.v + at);
             }
             if constexpr (kCodes) {
                 const char* pairs = (lane < kFewKeys ? p.cache.k_pairs : p.cache.v_pairs) + page * p.cache.pair_page_stride + slot * p.cache.pair_slot_stride + pair_head_at;
-                if constexpr (kGroups == 2) raw_pair = *reinterpret_cast<const u32x2*>(pairs);
-                else raw_pair[0] = *reinterpret_cast<const uint32_t*>(pairs);
+                if constexpr (kGroups == 2) raw.pair = *reinterpret_cast<const u32x2*>(pairs);
+                else raw.pair[0] = *reinterpret_cast<const uint32_t*>(pairs);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         };
         places(first_tile);
-        fetch();
-        places(first_tile + kStep);
+        fetch(first_tile + kStep);
 
         // ---- queries as the second operand: column = row of the result.  Product i takes channels 32 i + 8 quad + 0..7; in
         // 4 bits, of each 64, first the codes of 8 bytes' first dwords, then of the second: byte 8 quad + 4 (i % 2), with the
@@ -294,20 +301,20 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
         }
 
         for (uint32_t tile = first_tile; tile < last_tile; tile += kStep) {
-            const uint32_t seen = seen_next;
+            const uint32_t seen = raw.seen;
             uint32_t apart = 0;                         // one bit a key: one of its values' steps is above kStepMost
             float apart_step[kGroups];                  // lanes from 32 on: these steps, others 0
             // rows to LDS; values (in 4 bits: pairs) that are not there as zeros
             if (!kCodes && seen != ~0u) {
 #pragma unroll
                 for (uint32_t i = 0; i < kLoads; ++i)
-                    if (!((seen >> (i * kRowsAtOnce + load_row)) & 1u)) raw_v[i] = u32x4{0, 0, 0, 0};
+                    if (!((seen >> (i * kRowsAtOnce + load_row)) & 1u)) raw.v[i] = u32x4{0, 0, 0, 0};
             }
 #pragma unroll
             for (uint32_t i = 0; i < kLoads; ++i) {
                 const uint32_t key = i * kRowsAtOnce + load_row;
-                *reinterpret_cast<u32x4*>(k_lds + k_at(key, load_piece)) = raw_k[i];
-                *reinterpret_cast<u32x4*>(v_lds + v_at(key, load_piece)) = raw_v[i];
+                *reinterpret_cast<u32x4*>(k_lds + k_at(key, load_piece)) = raw.k[i];
+                *reinterpret_cast<u32x4*>(v_lds + v_at(key, load_piece)) = raw.v[i];
             }
             if constexpr (kCodes) {
                 const bool there = (seen >> (lane % kFewKeys)) & 1u;
@@ -315,7 +322,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
                 bool larger = false;
 #pragma unroll
                 for (uint32_t g = 0; g < kGroups; ++g) {
-                    par[2 * g] = there ? low16<E>(raw_pair[g]) : 0.0f, par[2 * g + 1] = there ? high16<E>(raw_pair[g]) : 0.0f;
+                    par[2 * g] = there ? low16<E>(raw.pair[g]) : 0.0f, par[2 * g + 1] = there ? high16<E>(raw.pair[g]) : 0.0f;
                     const float step = fabsf(par[2 * g]);
                     const bool out = lane >= kFewKeys && step < INFINITY && step >= kStepMost<E>;
                     apart_step[g] = out ? par[2 * g] : 0.0f;
@@ -354,8 +361,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kTi
                 if constexpr (kGroups == 2) *reinterpret_cast<f32x4*>(to) = f32x4{par[0], par[1], par[2], par[3]};
                 else *reinterpret_cast<f32x2*>(to) = f32x2{par[0], par[1]};
             }
-            fetch();
-            places(tile + 2 * kStep);
+            fetch(tile + 2 * kStep);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             int32_t base, end;
             tile_at<kFewKeys>(sp, tile, base, end);

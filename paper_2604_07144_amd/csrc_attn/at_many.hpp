@@ -22,7 +22,7 @@ constexpr float kHeadroom = 8.0f;
 template <typename P> constexpr float kWeightUp = std::is_same_v<P, fp16> ? 7.0f : 0.0f;
 
 // A cache in 4 bits is decoded to fp16, whose 11 bits keep codes of 4 on a lowest value and step of 8 where bf16 would round
-// them away (error of a chunk's results 0.0039 -> REL, against 0.0017 of the final rounding alone).  With bf16 pairs that
+// them away (a chunk's results were off by 0.0039 of themselves, and are by 0.0017, which is the final rounding).  With bf16 pairs that
 // holds a tile whose groups all lie, by their largest magnitude, from 2^-5 up to 2^14 (keys) and 2^8 (values), or are zero:
 // what fp16 then loses is below 2^-20 of the group.  Any other tile is decoded to bf16 and multiplied as that.
 constexpr float kGroupLeast = 0.03125f, kKeyMost = 16384.0f, kValueMost = 256.0f;
@@ -70,6 +70,11 @@ __device__ __forceinline__ float sum_halves(float x) {
 __device__ __forceinline__ void load_to_lds(const char* from, const void* to) {
     const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)to);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(at), "v"(from) : "memory");
+}
+// 16 bytes at an address that came through LDS, from which the compiler cannot tell that it lies in memory: a load that may be
+// either holds up the waits for LDS until it is there.
+__device__ __forceinline__ u32x4 load_global(const char* from) {
+    return *(__attribute__((address_space(1))) const u32x4*)(uintptr_t)from;
 }
 __device__ __forceinline__ void wait_loads() {
     __builtin_amdgcn_s_waitcnt(0x0F70);                     // vmcnt(0); the compiler knows of it, and waits for none of its own loads again
@@ -205,8 +210,8 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
             const char *at_k = lds_at_k[buf][code_key], *at_v = lds_at_v[buf][code_key];
             raw_k = raw_v = u32x4{0, 0, 0, 0};
             if (at_k) {
-                raw_k = *reinterpret_cast<const u32x4*>(at_k + 16 * code_piece);
-                raw_v = *reinterpret_cast<const u32x4*>(at_v + 16 * code_piece);
+                raw_k = load_global(at_k + 16 * code_piece);
+                raw_v = load_global(at_v + 16 * code_piece);
             }
         }
     };
@@ -252,11 +257,14 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
     put(0);
     wait_loads();
     __syncthreads();
-    for (uint32_t tile = first_tile; tile < last_tile; ++tile) {
+    auto odd_at = [&](uint32_t tile) { return uniform(lds_odd[(tile - first_tile) & 3u]); };
+    auto step = [&](auto type, uint32_t tile) {
+        using T = decltype(type);                           // what the tile is multiplied in; other than P only with queries as they were given
+        constexpr bool kGiven = !std::is_same_v<T, P>;
         const uint32_t buf = (tile - first_tile) & 1u;
         const uint64_t seen_all = lds_seen[(tile - first_tile) & 3u];
         const uint32_t seen_lo = __builtin_amdgcn_readfirstlane((uint32_t)seen_all), seen_hi = __builtin_amdgcn_readfirstlane((uint32_t)(seen_all >> 32));
-        const uint32_t odd = kCodes ? uniform(lds_odd[(tile - first_tile) & 3u]) : 1u;
+        const bool odd = kMixed ? kGiven : !kCodes || odd_at(tile) != 0;
         if (tile + 1 < last_tile) fetch(buf ^ 1u);
         const uint32_t turn = tile - first_tile;
         const bool puts = ((turn + kManyWaves - (kLookAhead - 2)) & (kManyWaves - 1)) == wave;
@@ -308,9 +316,7 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
             }
         }
         // work, unless all of the tile lies after the wavefront's rows or before their windows
-        auto work = [&](auto type) {
-            using T = decltype(type);
-            constexpr bool kGiven = !std::is_same_v<T, P>;  // queries as they were given, from memory: seldom needed, no registers
+        if (base <= pos_last && !(p.window && !sink_part && (uint32_t)base >= p.sinks && (int64_t)base + kManyKeys - 1 <= (int64_t)pos_first - p.window)) {
             const float unit = kGiven ? p.scale_log2 : q_unit;
             auto query = [&](uint32_t i) {
                 if constexpr (!kGiven) return q[i];
@@ -395,19 +401,19 @@ __global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) v
                     const u32x2 lo = lds_transposed(at + 16 * t * (2 * D)), hi = lds_transposed(at + (16 * t + 8) * (2 * D));
                     o[i] = mfma32<T>(u32x4{lo[0], lo[1], hi[0], hi[1]}, w[t], o[i]);
                 }
-        };
-        if (base <= pos_last && !(p.window && !sink_part && (uint32_t)base >= p.sinks && (int64_t)base + kManyKeys - 1 <= (int64_t)pos_first - p.window)) {
-            if constexpr (kMixed) {
-                if (odd) work(E{});
-                else work(P{});
-            } else {
-                work(P{});
-            }
         }
         if (tile + 1 < last_tile) put(turn + 1);
         if (puts) put_places(turn + 2);
         wait_loads();
         __syncthreads();
+    };
+    if constexpr (kMixed) {                                 // loops of their own, so that neither moves the other's registers
+        for (uint32_t tile = first_tile; tile < last_tile;) {
+            for (; tile < last_tile && !odd_at(tile); ++tile) step(P{}, tile);
+            for (; tile < last_tile && odd_at(tile); ++tile) step(E{}, tile);
+        }
+    } else {
+        for (uint32_t tile = first_tile; tile < last_tile; ++tile) step(P{}, tile);
     }
 
     const float total = sum_halves(l);

@@ -85,8 +85,8 @@ __device__ __forceinline__ int exponent_above(float x) { return (int)(__float_as
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126: 0
 
 // Joins the parts of a row, which lie at `at(0)` .. `at(n - 1)`.  Each lane has the (m, l) of a part; then 16 lanes read the
-// channels of a part, four parts at a time and four such rounds in flight, so that a row costs three trips to memory
-// however many parts it has (up to 16).
+// channels of a part, four parts at a time and four such rounds in flight, with the (m, l), so that a row costs two trips to
+// memory however many parts it has (up to 16).
 template <typename E, uint32_t D, typename F>
 __device__ __forceinline__ void join_row(const float* __restrict__ o, const f32x2* __restrict__ ml, F at, uint32_t n, char* dst) {
     constexpr uint32_t kPer = D / 16;                       // channels of a lane
@@ -97,6 +97,16 @@ __device__ __forceinline__ void join_row(const float* __restrict__ o, const f32x
     for (uint32_t z0 = 0; z0 < n; z0 += kLanes) {
         const uint32_t here_n = min(n - z0, kLanes);
         const f32x2 mine = lane < here_n ? ml[at(z0 + lane)] : f32x2{-INFINITY, 0.0f};
+        f32x4 x[4][kPer / 4];
+        auto load = [&](uint32_t z) {
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const f32x4* src = reinterpret_cast<const f32x4*>(o + at(z0 + min(z + 4 * i + set, here_n - 1)) * D + c0);
+#pragma unroll
+                for (uint32_t c = 0; c < kPer / 4; ++c) x[i][c] = src[c];
+            }
+        };
+        load(0);
         float grown = mine[0];
 #pragma unroll
         for (uint32_t m = 1; m < kLanes; m *= 2) grown = fmaxf(grown, __shfl_xor(grown, m));
@@ -107,13 +117,7 @@ __device__ __forceinline__ void join_row(const float* __restrict__ o, const f32x
 #pragma unroll
         for (uint32_t c = 0; c < kPer; ++c) acc[c] *= keep;
         for (uint32_t z = 0; z < here_n; z += 16) {
-            f32x4 x[4][kPer / 4];
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) {
-                const f32x4* src = reinterpret_cast<const f32x4*>(o + at(z0 + min(z + 4 * i + set, here_n - 1)) * D + c0);
-#pragma unroll
-                for (uint32_t c = 0; c < kPer / 4; ++c) x[i][c] = src[c];
-            }
+            if (z) load(z);
 #pragma unroll
             for (uint32_t i = 0; i < 4; ++i) {
                 const float f = __shfl(weight, z + 4 * i + set);     // 0 beyond the last part
