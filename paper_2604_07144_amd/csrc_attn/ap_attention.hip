@@ -88,7 +88,7 @@ struct Plan {
     uint64_t plan_bytes, bytes;
 };
 
-constexpr uint32_t kCus = 256, kResident = 2 * kCus;   // workgroups that the chip holds of the kernel of many rows: two on each CU
+constexpr uint32_t kCus = 256;
 
 // Workgroups on a CU of the kernel of few rows on the line, which a wavefront's share of it has to be worth: with 64 channels in
 // 4 bits four on a SIMD against two take 0.84 to 0.94 of the time where each has 12 to 24 places, 0.99 to 1.02 with 3.4 to 6,
@@ -111,6 +111,26 @@ uint32_t per_cu(uint32_t d, uint32_t bits, uint32_t tiles, uint64_t units) {
 constexpr uint32_t kTeamPairs = 256, kTeamTiles = 16, kTeamTilesOfFew = 32, kFewPairs = 128;
 constexpr uint32_t kUncutTiles = 5, kUncutTilesOfMany = 8, kManyPairs = 512;
 constexpr uint32_t kFewLeast = 2;        // places of the line that a wavefront of the kernel of few rows takes at least
+
+// Into how many chunks the keys of each tile of rows are cut: where the workgroups (tiles of rows times heads) do not fill the
+// chip, more of them are faster until joining costs more.  Estimated from what was measured (one chunk of 1024 tokens over 8192,
+// 32 heads on 8, 128 channels, of 1 to 4 sequences, so 256 to 1024 workgroups: 227, 309, 519, 584 us): a tile of keys takes a
+// workgroup kTileUs with the CU full of them, and 0.4 and a share of 0.6 of that with fewer; parts are written and read
+// at about 4 TB/s, and joining them is a launch more.
+uint32_t chunks_of(uint32_t d, uint32_t bits, uint64_t groups, uint32_t tiles, uint64_t rows) {
+    constexpr double kTileUs = 2.4, kEnterTiles = 3, kLaunchUs = 5, kPartBytesPerUs = 4e6;
+    constexpr uint32_t kLeastTiles = 8, kMostChunks = 64;
+    uint32_t on_cu = 0, best = 1;
+    for_dim(d, [&](auto dim) { for_bits(bits, [&](auto b) { on_cu = kManyPerCu<dim(), b()>; }); });
+    double least = 0;
+    for (uint32_t n = 1; n <= kMostChunks && (n == 1 || tiles >= n * kLeastTiles); ++n) {
+        const uint64_t all = groups * n, full = all / (kCus * on_cu), rest = all % (kCus * on_cu);
+        const double rounds = (double)full + (rest ? 0.4 + 0.6 * (double)((rest + kCus - 1) / kCus) / on_cu : 0.0);
+        const double us = rounds * ((tiles + n - 1) / n + kEnterTiles) * kTileUs + (n > 1 ? kLaunchUs + 2.0 * (double)n * (double)rows * (4.0 * d + 8) / kPartBytesPerUs : 0.0);
+        if (n == 1 || us < least) least = us, best = n;
+    }
+    return best;
+}
 
 ap_status plan_of(const ap_kv_cache* c, const Batch& b, uint32_t q_heads, uint32_t window, uint32_t sinks, Plan* out) {
     Plan r{};
@@ -143,9 +163,9 @@ ap_status plan_of(const ap_kv_cache* c, const Batch& b, uint32_t q_heads, uint32
     if (r.many) {
         r.row_tiles = (uint32_t)((uint64_t)b.n_tokens * group / kManyRows) + b.n_seqs;
         const uint32_t tiles = most_tiles(b, window, sinks, kManyRows / group + 2, kManyKeys);
-        const uint64_t groups = ((uint64_t)b.n_tokens * group / kManyRows + 1) * c->kv_heads;
-        const uint64_t chunks = std::max<uint64_t>(1, kResident / groups);
-        r.many_chunk = (uint32_t)std::max<uint64_t>(8, (tiles + chunks - 1) / chunks);
+        const uint64_t groups = ((uint64_t)b.n_tokens * group + kManyRows - 1) / kManyRows * c->kv_heads;
+        const uint32_t chunks = chunks_of(c->head_dim, c->bits, groups, tiles, (uint64_t)b.n_tokens * q_heads);
+        r.many_chunk = (tiles + chunks - 1) / chunks;
         r.many_chunks = (tiles + r.many_chunk - 1) / r.many_chunk;
         if (((uint64_t)r.row_tiles) * c->kv_heads * r.many_chunks >= kMostGroups) return AP_ERR_RANGE;
         if (r.many_chunks > 1) {

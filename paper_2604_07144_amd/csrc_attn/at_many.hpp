@@ -86,10 +86,13 @@ __device__ __forceinline__ void wait_loads() {
 template <uint32_t D> __device__ __forceinline__ uint32_t key_piece(uint32_t key, uint32_t c) { return D == 128 ? c ^ (key & 15u) : c ^ ((key >> 1) & 7u); }
 template <uint32_t D> __device__ __forceinline__ uint32_t value_piece(uint32_t key, uint32_t c) { return D == 128 ? c ^ ((key & 3u) << 2) : c ^ (((key >> 1) & 1u) << 2); }
 
+// Workgroups that registers leave room for on a CU.
+template <uint32_t D, uint32_t kBits> constexpr uint32_t kManyPerCu = D == 128 ? 2 : kBits == 16 ? 4 : 3;
+
 // Workgroups: [tile of rows, last first][chunk][kv head]: late rows see most keys, and the heads of a tile, whose keys
 // are other memory, spread over the XCDs while all tiles of a head stay on one.
 template <typename E, uint32_t D, uint32_t kBits>
-__global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : kBits == 16 ? 4 : 3) void k_attend_many(const AttnParams p, const uint32_t n_row_tiles, const uint32_t n_chunks) {
+__global__ __launch_bounds__(kManyThreads, (kManyPerCu<D, kBits>)) void k_attend_many(const AttnParams p, const uint32_t n_row_tiles, const uint32_t n_chunks) {
     constexpr uint32_t kSteps = D / 16, kOut = D / 32, kPieces = D / 8;
     constexpr bool kCodes = kBits == 4;
     using P = std::conditional_t<kCodes, fp16, E>;          // what ordinary tiles are multiplied in
