@@ -82,9 +82,10 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // Where 16-byte piece `c` of a key's (value's) row lies in LDS, in its row.  Keys: the 16 rows that a read takes at once
-// hold the same piece in 16 different places.  Values: the 64 bytes of 4 rows that a transposing read takes at once likewise.
+// hold the same piece in 16 different places.  Values: the 64 bytes of 4 rows that a transposing read takes at once likewise,
+// and so do neighbouring rows of which decoded pieces of one number are written at once.
 template <uint32_t D> __device__ __forceinline__ uint32_t key_piece(uint32_t key, uint32_t c) { return D == 128 ? c ^ (key & 15u) : c ^ ((key >> 1) & 7u); }
-template <uint32_t D> __device__ __forceinline__ uint32_t value_piece(uint32_t key, uint32_t c) { return D == 128 ? c ^ ((key & 3u) << 2) : c ^ (((key >> 1) & 1u) << 2); }
+template <uint32_t D> __device__ __forceinline__ uint32_t value_piece(uint32_t key, uint32_t c) { return D == 128 ? c ^ (key & 3u) * 5u : c ^ ((key >> 1) & 1u) * 5u; }
 
 // Workgroups that registers leave room for on a CU.
 template <uint32_t D, uint32_t kBits> constexpr uint32_t kManyPerCu = D == 128 ? 2 : kBits == 16 ? 4 : 3;
@@ -109,8 +110,19 @@ __global__ __launch_bounds__(kManyThreads, (kManyPerCu<D, kBits>)) void k_attend
 
     // Sequence s has the row tiles from first[s] * group / kManyRows + s on up to the next one's, which is never too few.
     auto begins = [&](uint32_t i) { return (uint32_t)((uint64_t)(uint32_t)p.batch.first[i] * p.group / kManyRows) + i; };
-    const uint32_t s = uniform(count_to(p.batch.n_seqs - 1, slot, begins)), slot0 = uniform(begins(s));
-    Seq seq = seq_at(p.batch, s);
+    uint32_t s, slot0;
+    Seq seq;
+    if (p.batch.n_seqs <= kLanes) {                         // a lane each, lengths and all in one trip to memory
+        const uint32_t i = min(lane, p.batch.n_seqs - 1), first = begins(i);
+        const Seq mine = seq_at(p.batch, i);
+        s = uniform((uint32_t)__popcll(__ballot(lane > 0 && lane < p.batch.n_seqs && first <= slot)));
+        slot0 = __builtin_amdgcn_readlane(first, s);
+        seq = Seq{(int32_t)__builtin_amdgcn_readlane(mine.first, s), (int32_t)__builtin_amdgcn_readlane(mine.n_new, s),
+                  (int32_t)__builtin_amdgcn_readlane(mine.kv_len, s), (int32_t)__builtin_amdgcn_readlane(mine.pos0, s)};
+    } else {
+        s = uniform(count_to(p.batch.n_seqs - 1, slot, begins)), slot0 = uniform(begins(s));
+        seq = seq_at(p.batch, s);
+    }
     seq = Seq{uniform(seq.first), uniform(seq.n_new), uniform(seq.kv_len), uniform(seq.pos0)};
     const int32_t n_new = min(seq.n_new, (int32_t)p.batch.max_new);
     const uint32_t rows = (uint32_t)n_new * p.group;
