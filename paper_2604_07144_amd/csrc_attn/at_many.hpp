@@ -24,7 +24,7 @@ template <typename P> constexpr float kWeightUp = std::is_same_v<P, fp16> ? 7.0f
 // A cache in 4 bits is decoded to fp16, whose 11 bits keep codes of 4 on a lowest value and step of 8 where bf16 would round
 // them away (a chunk's results were off by 0.0039 of themselves, and are by 0.0017, which is the final rounding).  With bf16 pairs that
 // holds a tile whose groups all lie, by their largest magnitude, from 2^-5 up to 2^14 (keys) and 2^8 (values), or are zero:
-// what fp16 then loses is below 2^-20 of the group.  Any other tile is decoded to bf16 and multiplied as that.
+// what fp16 then loses by its range is below 2^-16 of the group.  Any other tile is decoded to bf16 and multiplied as that.
 constexpr float kGroupLeast = 0.03125f, kKeyMost = 16384.0f, kValueMost = 256.0f;
 template <typename E> __device__ __forceinline__ bool ordinary(uint32_t key_pair, uint32_t value_pair) {
     auto most = [](uint32_t pr) { return fmaxf(fabsf(high16<E>(pr)), fabsf(fmaf(15.0f, low16<E>(pr), high16<E>(pr)))) + 0.0f * low16<E>(pr); };
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(kManyThreads, (kManyPerCu<D, kBits>)) void k_attend
             }
         const int e = max(exponent_above(max_halves(most)), -100);
         const float up = power2(14 - e);
-        q_unit *= power2(e - 14);
+        q_unit = fmaxf(q_unit * power2(e - 14), 1.17549435e-38f);      // not 0, which would make NaN of what is hidden by minus infinity; scores are as good as 0 there
 #pragma unroll
         for (uint32_t i = 0; i < kSteps; ++i)
 #pragma unroll
@@ -345,7 +345,11 @@ __global__ __launch_bounds__(kManyThreads, (kManyPerCu<D, kBits>)) void k_attend
             for (uint32_t t = 0; t < 2; ++t)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) sc[t][j] = 0.0f;
+            // Which wavefront of a SIMD goes first matters where one has products to give out: with 128 channels the first product's
+            // (0.99 of the time over calls of many kinds, 0.94 to 1.02), with 64 the second's with its exponentials (0.97, 0.95 to 0.99);
+            // the other way round 0.985 (0.88 to 1.10) and 0.995.
             // pieces are told apart by exclusive or, so one number and the product's give the place
+            if constexpr (D == 128) __builtin_amdgcn_s_setprio(1);
             const uint32_t key_at = here(col * (2 * D) + key_piece<D>(col, half) * 16);
 #pragma unroll
             for (uint32_t i = 0; i < kSteps; ++i) {
@@ -363,6 +367,7 @@ __global__ __launch_bounds__(kManyThreads, (kManyPerCu<D, kBits>)) void k_attend
             }
             __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
 
+            if constexpr (D == 128) __builtin_amdgcn_s_setprio(0);
             // what is not seen: keys that are not there (any row), keys after a row or before its window
             const bool each = base + (int32_t)kManyKeys - 1 > pos_first || (p.window && !sink_part && (int64_t)base <= (int64_t)pos_last - p.window);
             if (each || (seen_lo & seen_hi) != ~0u) {
@@ -397,6 +402,7 @@ __global__ __launch_bounds__(kManyThreads, (kManyPerCu<D, kBits>)) void k_attend
                     for (int j = 0; j < 16; ++j) o[i][j] *= keep;
             }
             const float from = m == -INFINITY ? 0.0f : m - kWeightUp<P>;
+            if constexpr (D == 64) __builtin_amdgcn_s_setprio(1);
             u32x4 w[4];                                     // weights of 16 keys each, as the second product takes them
 #pragma unroll
             for (uint32_t t = 0; t < 2; ++t)
@@ -417,6 +423,7 @@ __global__ __launch_bounds__(kManyThreads, (kManyPerCu<D, kBits>)) void k_attend
                     o[i] = mfma32<T>(u32x4{lo[0], lo[1], hi[0], hi[1]}, w[t], o[i]);
                 }
         }
+        if constexpr (D == 64) __builtin_amdgcn_s_setprio(0);
         if (tile + 1 < last_tile) put(turn + 1);
         if (puts) put_places(turn + 2);
         wait_loads();

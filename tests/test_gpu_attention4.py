@@ -109,3 +109,9 @@ def test_steps_that_stand_apart(dtype, by, d, new):
         for s in range(3):                                  # seen by the last token only
             r.vp[int(r.table[s, (held[s] - 1) // 20]), :, (held[s] - 1) % 20] *= by
         check(r.attend(q, 0.09), *r.expected(q, 0.09))
+
+
+def test_queries_of_zeros_with_a_tiny_scale():
+    r = Replica([150], [150], K=1, A=4, bits=4)
+    q = torch.zeros((r.T, r.A, r.d), dtype=r.dtype, device="cuda")
+    check(r.attend(q, 1e-20), *r.expected(q, 1e-20))
