@@ -90,14 +90,20 @@ struct Plan {
 
 constexpr uint32_t kCus = 256;
 
-// Workgroups on a CU of the kernel of few rows on the line, which a wavefront's share of it has to be worth: with 64 channels in
-// 4 bits four on a SIMD against two take 0.84 to 0.94 of the time where each has 12 to 24 places, 0.99 to 1.02 with 3.4 to 6,
-// and 1.17 with 3.  (16 bits with 64 channels, and 4 bits with 128, lose 1.03 to 1.25 by a third one.)
-constexpr uint32_t kPlacesOfFour = 8;
+// Workgroups on a CU of the kernel of few rows on the line.  Those of kFewDoubles take all that fit where a wavefront's share of
+// the line stays kLeastPlaces, otherwise half as many, which leave less to join.  64 channels, up to 16 rows, four on a SIMD
+// against two: 0.84 to 0.94 of the time with 12 to 24 places each, 0.99 to 1.02 with 3.4 to 6, 1.17 with 3; 128 channels,
+// up to 32 rows, two against one: 0.70 to 0.82 with 12 places and more, 0.94 to 1.04 with 5 to 10, 1.20 with 3.  (A third one
+// costs 16 bits with 64 channels 1.04 and 4 bits with 128 channels and 16 rows 1.2 of the time.)
+constexpr uint32_t kLeastPlaces = 8;
 uint32_t per_cu(uint32_t d, uint32_t bits, uint32_t tiles, uint64_t units) {
     uint32_t n = 0;
-    for_dim(d, [&](auto dim) { for_bits(bits, [&](auto b) { n = tiles == 1 ? kFewPerSimd<dim(), b(), 1, false> : kFewPerSimd<dim(), b(), 2, false>; }); });
-    return n == 4 && units < (uint64_t)kPlacesOfFour * 4 * kCus * kLineWaves ? 2 : n;
+    bool doubles = false;
+    auto of = [&](auto dim, auto b, auto t) { n = kFewPerSimd<dim(), b(), t(), false>, doubles = kFewDoubles<dim(), b(), t(), false>; };
+    for_dim(d, [&](auto dim) {
+        for_bits(bits, [&](auto b) { tiles == 1 ? of(dim, b, std::integral_constant<uint32_t, 1>{}) : of(dim, b, std::integral_constant<uint32_t, 2>{}); });
+    });
+    return doubles && units < (uint64_t)kLeastPlaces * n * kCus * kLineWaves ? n / 2 : n;
 }
 
 // How the kernel of few rows deals out its work.  32 heads on 8, 128 channels, bf16, sequences of one length, us:

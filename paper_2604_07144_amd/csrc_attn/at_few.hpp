@@ -75,9 +75,12 @@ struct FewSeq {
 template <uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
 constexpr uint32_t kFewWaves = kTeam && !(D == 128 && kBits == 16 && kTiles == 2) ? 8 : 4;
 
+// Variants of the line (4 bits) that run with twice the wavefronts on a SIMD where each still has a good share of the line.
+template <uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
+constexpr bool kFewDoubles = kBits == 4 && !kTeam && (D == 64 ? kTiles == 1 : kTiles == 2);
 // Wavefronts that registers leave room for on a SIMD.
 template <uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
-constexpr uint32_t kFewPerSimd = kTiles == 2 && D == 128 && (kBits == 16 || !kTeam) ? 1 : kTiles == 1 && D == 64 && kBits == 4 && !kTeam ? 4 : 2;
+constexpr uint32_t kFewPerSimd = D == 128 && kBits == 16 && kTiles == 2 ? 1 : D == 64 && kFewDoubles<D, kBits, kTiles, kTeam> ? 4 : 2;
 
 // kTiles: tiles of 16 rows.  kTeam: a workgroup takes a (sequence, head) and joins its wavefronts' parts itself.
 template <typename E, uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
