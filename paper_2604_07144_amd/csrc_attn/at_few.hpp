@@ -326,22 +326,24 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
 #pragma unroll
                 for (uint32_t g = 0; g < kGroups; ++g) {
                     par[2 * g] = there ? low16<E>(raw.pair[g]) : 0.0f, par[2 * g + 1] = there ? high16<E>(raw.pair[g]) : 0.0f;
-                    const float step = fabsf(par[2 * g]);
-                    const bool out = lane >= kFewKeys && step < INFINITY && step >= kStepMost<E>;
-                    apart_step[g] = out ? par[2 * g] : 0.0f;
-                    larger |= lane >= kFewKeys && step < kStepMost<E> && step >= power2(step_exp);
+                    larger |= lane >= kFewKeys && fabsf(par[2 * g]) >= power2(step_exp);
+                    apart_step[g] = 0.0f;
                 }
-                bool out = apart_step[0] != 0.0f;
-                if constexpr (kGroups == 2) out |= apart_step[kGroups - 1] != 0.0f;
-                apart = (uint32_t)(__ballot(out) >> kFewKeys);
                 if (__any(larger)) {                    // a larger step than any so far (the first steps do this, seldom others)
                     float most = 0.0f;
 #pragma unroll
-                    for (uint32_t g = 0; g < kGroups; ++g)
-                        if (lane >= kFewKeys && fabsf(par[2 * g]) < kStepMost<E>) most = fmaxf(most, fabsf(par[2 * g]));
+                    for (uint32_t g = 0; g < kGroups; ++g) {
+                        const float size = fabsf(par[2 * g]);
+                        if (lane < kFewKeys) continue;
+                        if (size < kStepMost<E>) most = fmaxf(most, size);
+                        else if (size < INFINITY) apart_step[g] = par[2 * g], par[2 * g] = 0.0f;
+                    }
+                    bool out = apart_step[0] != 0.0f;
+                    if constexpr (kGroups == 2) out |= apart_step[kGroups - 1] != 0.0f;
+                    apart = (uint32_t)(__ballot(out) >> kFewKeys);
 #pragma unroll
                     for (uint32_t x = 1; x < kLanes; x *= 2) most = fmaxf(most, __shfl_xor(most, x));
-                    const int e = __builtin_amdgcn_readfirstlane(exponent_above(most));
+                    const int e = max(__builtin_amdgcn_readfirstlane(exponent_above(most)), step_exp);
                     const float down = power2(max(step_exp - e, -126));
                     step_exp = e;
 #pragma unroll
@@ -355,10 +357,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
                 if (lane >= kFewKeys) {                 // values: step in the weights' scale, and what the middle code stands for
                     const float f = power2(kWeightExponent - step_exp);
 #pragma unroll
-                    for (uint32_t g = 0; g < kGroups; ++g) {
-                        if (apart_step[g] != 0.0f) par[2 * g] = 0.0f;
-                        par[2 * g + 1] = fmaf(8.0f, par[2 * g], par[2 * g + 1]), par[2 * g] *= f;
-                    }
+                    for (uint32_t g = 0; g < kGroups; ++g) par[2 * g + 1] = fmaf(8.0f, par[2 * g], par[2 * g + 1]), par[2 * g] *= f;
                 }
                 float* to = (lane < kFewKeys ? k_par : v_par) + (lane % kFewKeys) * kPairFloats;
                 if constexpr (kGroups == 2) *reinterpret_cast<f32x4*>(to) = f32x4{par[0], par[1], par[2], par[3]};
