@@ -21,6 +21,11 @@
 //    the two halves of bytes is all the conversion there is.  Scores are step * (codes . q) + lo * (sum of q), per group of
 //    64 channels; for values each weight is multiplied by the key's step before its one rounding, and lo is summed apart
 //    in 32 bits.  So neither keys nor values are rounded at all.
+//
+// Measured, one token, 128 channels, bf16: 64 sequences of 4096 to 8192, 32 heads of their own 6.0 TB/s in 16 bits and 5.3 in 4;
+// with 32 heads on 8 5.7 and 4.5.  Shorter batches pay 5 us for the launch that joins, and 4 bits are bound by instructions
+// there: about 380 a tile of 32 keys, 55 % of what the SIMDs give out, so 64 slots with bimodal lengths take 36 to 38 us
+// (3.1 TB/s) where 16 bits take 88 (4.6).
 #ifndef AT_FEW_HPP
 #define AT_FEW_HPP
 
