@@ -48,3 +48,11 @@ def test_sequences_around_a_wavefront(n):
     held[-1] = new[-1] = 0
     new[n // 2], held[n // 2] = 70, 75
     _check(Replica(held, new, K=1, A=2, page=8, d=64))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("window, sinks", [(0, 0), (50, 3)])
+def test_whole_prompts_with_single_tokens_among_them(window, sinks, bits):
+    """Prompts down to one token, and one new token of a sequence that is as long as the longest prompt."""
+    held, new = [200, 1, 130, 3, 77, 0, 200, 9], [200, 1, 130, 3, 77, 0, 1, 9]
+    _check(Replica(held, new, K=2, A=4, bits=bits, page=20), window, sinks)
