@@ -100,6 +100,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
     constexpr uint32_t kPairFloats = 2 * kGroups;           // (step, lo) of a key
     // A maximum is only raised when a score passes it by 2^this; in 4 bits and fp16 that comes off the weights' range.
     constexpr float kFewHeadroom = kCodes && std::is_same_v<E, fp16> ? 4.0f : 8.0f;
+    constexpr float kUp = kCodes ? 0.0f : kWeightUp<E>;     // (codes have their own, with the step)
     constexpr int kWeightExponent = std::is_same_v<E, fp16> ? 10 : 100;
     constexpr uint32_t kWaveBytes = 2 * kSideBytes + (kCodes ? 2 * kFewKeys * kPairFloats * 4 : 0);
     constexpr uint32_t kOutStride = D + 4;                  // floats between rows where a team's results meet
@@ -456,7 +457,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
                         for (uint32_t g = 0; g < kGroups; ++g) eights[n][g] *= keep, lows[n][g] *= keep;
                     }
                 }
-                const float from = m[n] == -INFINITY ? 0.0f : m[n];
+                const float from = m[n] == -INFINITY ? 0.0f : m[n] - kUp;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     x[n][j] = exp2_of(x[n][j] - from);
@@ -651,7 +652,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
                     if (whole) *reinterpret_cast<u32x2*>(dst + 2 * c) = u32x2{pack2<E>(x[0], x[1]), pack2<E>(x[2], x[3])};
                     else *reinterpret_cast<f32x4*>(part + c) = x;
                 });
-                if (!whole && quad == 0) p.few_ml[at] = f32x2{m[n], sum};
+                if (!whole && quad == 0) p.few_ml[at] = f32x2{m[n] - kUp, sum};
             }
         }
     }

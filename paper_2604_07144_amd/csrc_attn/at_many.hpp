@@ -22,8 +22,6 @@
 namespace {
 
 constexpr float kHeadroom = 8.0f;
-// Weights in fp16 are held times 2^this: with the headroom their largest is 2^15, and none above 2^-31 of the maximum is lost.
-template <typename P> constexpr float kWeightUp = std::is_same_v<P, fp16> ? 7.0f : 0.0f;
 
 // A cache in 4 bits is decoded to fp16, whose 11 bits keep codes of 4 on a lowest value and step of 8 where bf16 would round
 // them away (a chunk's results were off by 0.0039 of themselves, and are by 0.0017, which is the final rounding).  With bf16 pairs that

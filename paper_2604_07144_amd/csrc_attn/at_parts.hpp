@@ -77,6 +77,10 @@ __device__ __forceinline__ bool not_finite16(uint32_t two, uint32_t exponent) {
 template <typename E> constexpr uint32_t kExponentStep = std::is_same_v<E, bf16> ? 0x00800080u : 0x04000400u;   // 1 in both exponents of a dword
 template <typename E> constexpr uint32_t kExponent = std::is_same_v<E, bf16> ? 0x7F80u : 0x7C00u;
 
+// Weights in fp16 are held times 2^this: with a headroom of 2^8 their largest is 2^15, and what is lost of a weight by the type's
+// range is below 2^-32 of the maximum's.
+template <typename P> constexpr float kWeightUp = std::is_same_v<P, fp16> ? 7.0f : 0.0f;
+
 // A power of two with the exponent e.
 __device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 // The exponent above x > 0: x < 2^e.
