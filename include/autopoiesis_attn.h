@@ -100,8 +100,9 @@ ap_status ap_kv_read(const ap_kv_cache *cache, const ap_seq_batch *batch, const 
  * A row that sees nothing (or only scores of minus infinity) is zero.  Keys and values that a row does not see do not
  * reach it, whatever they hold.  q_heads is a multiple of kv_heads: q head h reads key/value head h / (q_heads / kv_heads).
  * Scores, maxima and sums are in 32 bits; weights are rounded to 16 bits before they meet the values.  Weights are held up to
- * 2^15 times their size, so a row whose sum of values passes 2^112 can overflow to an infinity.  Values in 4 bits are used as
- * lo + step * code with at least the 16-bit type's precision.
+ * 2^15 times their size, so a row whose sum of values passes 2^112 can overflow to an infinity.  q . k, its parts and scale times
+ * it are numbers of 32 bits: where one overflows, the row can be NaN.  Values in 4 bits are used as lo + step * code with at least the 16-bit type's
+ * precision.
  *   scale     : finite and > 0.
  *   workspace : device memory of at least ap_attention_workspace bytes, aligned to 16 bytes (may be NULL where that
  *               is 0), for this call alone until it has run.

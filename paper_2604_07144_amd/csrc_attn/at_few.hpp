@@ -45,7 +45,7 @@ __device__ __forceinline__ u32x2 lds_transposed8(const char* at) {
 }
 
 template <typename E> constexpr int kCodeExponent = std::is_same_v<E, bf16> ? 133 : 24;      // a code n as bits: n * 2^-this
-template <typename E> constexpr int kOperandExponent = std::is_same_v<E, bf16> ? 100 : 14;   // the other operand is brought below 2^this
+template <typename E> constexpr int kOperandExponent = std::is_same_v<E, bf16> ? 125 : 14;   // the other operand is brought below 2^this
 // Steps of values from here on stay out of the products, so that no such step, which perhaps few rows see, takes the others'
 // weights out of the operand's range.
 template <typename E> constexpr float kStepMost = std::is_same_v<E, bf16> ? 65536.0f : 8.0f;
@@ -254,12 +254,13 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
         // channels in spread()'s order and those that come times 16 divided by it.
         u32x4 q[kTiles][kSteps];
         int32_t pos[kTiles];                            // position of the column's token
-        float q_sum[kTiles][kGroups], q_scale[kTiles];
+        float q_sum[kTiles][kGroups], q_scale[kTiles], unit_of[kTiles];   // scores are in units of unit_of (1 in 16 bits), which is in powers of two
 #pragma unroll
         for (uint32_t n = 0; n < kTiles; ++n) {
             const uint32_t r = min(n * 16 + here(col), rows - 1), quad = here(lane) / 16, token = over_group(p, r);
             pos[n] = pos_first + (int32_t)token;
             const char* row = p.q.data + (int64_t)(seq_first + (int32_t)token) * p.q.token_stride + (int64_t)(head * p.group + r - token * p.group) * p.q.head_stride;
+            unit_of[n] = 1.0f;
             if constexpr (!kCodes) {
 #pragma unroll
                 for (uint32_t i = 0; i < kSteps; ++i) q[n][i] = *reinterpret_cast<const u32x4*>(row + 64 * i + 16 * quad);
@@ -272,23 +273,33 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
                     for (int j = 0; j < 4; ++j) x[i][2 * j] = low16<E>(y[j]), x[i][2 * j + 1] = high16<E>(y[j]);
                 }
 #pragma unroll
+                for (uint32_t i = 0; i < kSteps; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[i][j]));
+                most = max_column(most);
+                // The row is brought below 1 (the largest numbers below 4) by a power of two, so nothing is rounded that counts, and that
+                // goes into the unit of its scores together with the scale; what would take the unit out of range stays with the row.
+                const int e = most < INFINITY ? min(exponent_above(most), 126) : 0, e_scale = exponent_above(p.scale_log2);
+                const int e_unit = min(max(e, -100 - e_scale), 100 - e_scale), e_row = min(max(e - e_unit, -100), 100);
+                unit_of[n] = p.scale_log2 * power2(e_unit / 2) * power2(e_unit - e_unit / 2);
+                q_scale[n] = power2(kCodeExponent<E> - kOperandExponent<E> + e_row);
+#pragma unroll
                 for (uint32_t g = 0; g < kGroups; ++g) {
                     float sum = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) sum += x[2 * g + j / 8][j % 8], most = fmaxf(most, fabsf(x[2 * g + j / 8][j % 8]));
-                    q_sum[n][g] = sum_column(sum) * p.scale_log2;
+                    for (int j = 0; j < 16; ++j) {
+                        float& y = x[2 * g + j / 8][j % 8];
+                        y *= power2(-e);
+                        sum += y;
+                    }
+                    q_sum[n][g] = sum_column(sum) * power2(e_row);
                 }
-                most = max_column(most);
-                // the largest of the row is brought just below 2^kOperandExponent: a power of two, so nothing is rounded that counts
-                const int e = most < INFINITY ? max(exponent_above(most), -24) : 0;
-                const float up = power2(kOperandExponent<E> - e);
-                q_scale[n] = power2(kCodeExponent<E> - kOperandExponent<E>) * p.scale_log2 * power2(e / 2) * power2(e - e / 2);
 #pragma unroll
                 for (uint32_t i = 0; i < kSteps; ++i) {
                     constexpr int kOrder[8] = {0, 4, 1, 5, 2, 6, 3, 7};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float f = j % 2 ? up * 0.0625f : up;
+                        const float f = power2(kOperandExponent<E> - (j % 2 ? 4 : 0));
                         q[n][i][j] = pack2<E>(x[i][kOrder[2 * j]] * f, x[i][kOrder[2 * j + 1]] * f);
                     }
                 }
@@ -374,7 +385,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
             int32_t base, end;
             tile_at<kFewKeys>(sp, tile, base, end);
 
-            // scores (S^T = K Q^T), in powers of two; the lane has keys 4 quad + 0..3 of both halves for its column
+            // scores (S^T = K Q^T), in units of unit_of; the lane has keys 4 quad + 0..3 of both halves for its column
             float x[kTiles][8];
 #pragma unroll
             for (uint32_t r = 0; r < 2; ++r) {
@@ -444,7 +455,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
                 float top = x[n][0];
 #pragma unroll
                 for (int j = 1; j < 8; ++j) top = fmaxf(top, x[n][j]);
-                top = max_column(top);
+                top = max_column(top) * unit_of[n];
                 const bool raise = top > m[n] + kFewHeadroom || (m[n] == -INFINITY && top > m[n]);
                 if (__any(raise)) {
                     const float grown = raise ? top : m[n], keep = raise && m[n] != -INFINITY ? exp2_of(m[n] - grown) : 1.0f;
@@ -460,7 +471,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
                 const float from = m[n] == -INFINITY ? 0.0f : m[n] - kUp;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    x[n][j] = exp2_of(x[n][j] - from);
+                    x[n][j] = exp2_of(fmaf(x[n][j], unit_of[n], -from));
                     l[n] += x[n][j];
                 }
                 if constexpr (!kCodes) {

@@ -56,3 +56,52 @@ def test_many_small_weights_in_fp16(held, K, A, new, d):
     tokens = [0, new // 2, new - 1]
     want, tol = _rows(r, q, scale, tokens, own)
     check(r.attend(q, scale)[tokens], want, tol)
+
+
+def _code_rows(r, q, scale, tokens, window=0, sinks=0):
+    """Bounds for few rows over 4 bits, where codes are multiplied as they are and nothing but each weight, times its key's step, is rounded
+    to 16 bits.
+
+    A weight meets what its code is off the middle one, at most 8 steps, so its rounding is worth half a step of the type of that.  In
+    32 bits a score is put together of step * (codes . q) and lo * (sum of q), so what it is off by goes by the sum of |q| times
+    |lo| + 15 |step|, and a weight by twice that; the sums of values by what they have added up, 15 steps and |lo|.  fp16 holds weights
+    times their steps, 2^10 at the largest step, to half of 2^-24."""
+    pairs = {f: x.double().cpu().numpy() for f, x in (("k", r.kp), ("v", r.vp))}
+    held = np.isin(np.arange(r.n_pages), r.table[r.table >= 0])
+    step, lo = np.abs(pairs["v"][held][..., 0::2]).max(), np.abs(pairs["v"][held][..., 1::2]).max()
+    key = (np.abs(pairs["k"][held][..., 1::2]) + 15 * np.abs(pairs["k"][held][..., 0::2])).max()
+    u = torch.finfo(r.dtype).eps / 2
+    sums = np.abs(q.double().cpu().numpy()).sum(-1).max() * scale * key
+
+    def own(mean, seen, live, k, v):
+        moved = 2 * (r.d + 8) * 2.0 ** -24 * sums
+        lost = seen * 2.0 ** -31 * step if r.dtype == torch.float16 else 0.0
+        return 8 * step * u + mean * moved * (1 + moved) + (seen / 16 + 40) * 2.0 ** -24 * (15 * step + lo) + lost + (2.0 ** -25 if r.dtype == torch.float16 else 0.0)
+
+    return _rows(r, q, scale, tokens, own, window, sinks)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("K, A, new", [(1, 4, 1), (2, 2, 1), (1, 24, 1), (1, 4, 6)])
+@pytest.mark.parametrize("dtype, k_by, q_by, by", [
+    ("bf16", 1, 1, 1), ("fp16", 1, 1, 1), ("fp16", 2.0 ** -6, 2.0 ** 10, 2.0 ** -4), ("fp16", 8, 2.0 ** -8, 32), ("fp16", 1, 2.0 ** -9, 2.0 ** 9),
+    ("bf16", 2.0 ** -100, 2.0 ** 60, 2.0 ** 40), ("bf16", 2.0 ** -118, 2.0 ** 118, 1), ("bf16", 2.0 ** -118, 1, 2.0 ** 118), ("bf16", 2.0 ** 110, 2.0 ** -60, 2.0 ** -50),
+    ("bf16", 2.0 ** 100, 2.0 ** -100, 1), ("bf16", 1, 2.0 ** -120, 2.0 ** 120), ("bf16", 1, 2.0 ** 120, 2.0 ** -120), ("bf16", 2.0 ** -60, 2.0 ** -60, 2.0 ** 120)])
+def test_few_rows_over_4_bits_round_weights_only(dtype, k_by, q_by, by, K, A, new, d):
+    """Scores of ordinary size made of keys, queries and scales of any."""
+    for held in ([300, 77, 32], [4000, 2100, 700]):
+        r = Replica(held, [new] * 3, K=K, A=A, d=d, dtype=dtype, bits=4, page=20)
+        r.kp.copy_(r.kp.float() * k_by)
+        q = (r.made(r.T, r.A, r.d) * q_by).to(r.dtype)
+        tokens, scale = [0, new, 3 * new - 1], d ** -0.5 * by
+        check(r.attend(q, scale)[tokens], *_code_rows(r, q, scale, tokens))
+        check(r.attend(q, scale, 70, 3)[tokens], *_code_rows(r, q, scale, tokens, 70, 3))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("new", [1, 3, 60])
+def test_scales_that_leave_no_score(new, bits):
+    """A scale below the smallest normal number: every key that is seen has the same weight."""
+    r = Replica([200, 333], [new, new], K=1, A=4, bits=bits)
+    q = r.made(r.T, r.A, r.d).to(r.dtype)
+    check(r.attend(q, 1e-42, 90, 2), *r.expected(q, 1e-42, 90, 2))
