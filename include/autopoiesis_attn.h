@@ -103,7 +103,7 @@ ap_status ap_kv_read(const ap_kv_cache *cache, const ap_seq_batch *batch, const 
  * 2^15 times their size, so a row whose sum of values passes 2^112 can overflow to an infinity.  q . k, its parts and scale times
  * it are numbers of 32 bits: where one overflows, the row can be NaN.  Values in 4 bits are used as lo + step * code with at least the 16-bit type's
  * precision.
- *   scale     : finite and > 0.
+ *   scale     : > 0, and log2(e) times it finite.
  *   workspace : device memory of at least ap_attention_workspace bytes, aligned to 16 bytes (may be NULL where that
  *               is 0), for this call alone until it has run.
  * Results do not depend on timing.  Errors as above; a workspace that is too small is AP_ERR_INVALID. */

@@ -270,7 +270,8 @@ ap_status ap_attention(const ap_kv_cache* cache, const ap_seq_batch* batch, cons
     if (st == AP_OK) st = take_rows(q, &p.q);
     if (st == AP_OK) st = take_rows(out, &p.out);
     if (st != AP_OK) return st;
-    if (q_heads == 0 || q_heads % cache->kv_heads || !(scale > 0.0f) || !std::isfinite(scale)) return AP_ERR_INVALID;
+    const float scale_log2 = scale * 1.44269504088896341f;
+    if (q_heads == 0 || q_heads % cache->kv_heads || !(scale > 0.0f) || !std::isfinite(scale_log2)) return AP_ERR_INVALID;
     st = plan_of(cache, p.batch, q_heads, window, sinks, &plan);
     if (st != AP_OK) return st;
     if (plan.bytes > 0 && (!workspace || !multiple(workspace, 16) || workspace_bytes < plan.bytes)) return AP_ERR_INVALID;
@@ -278,7 +279,7 @@ ap_status ap_attention(const ap_kv_cache* cache, const ap_seq_batch* batch, cons
     p.q_heads = q_heads, p.kv_heads = cache->kv_heads, p.group = q_heads / cache->kv_heads;
     divider(p.group, &p.group_magic, &p.group_shift);
     p.window = window, p.sinks = window ? sinks : 0;
-    p.scale_log2 = scale * 1.44269504088896341f;
+    p.scale_log2 = scale_log2;
     p.few_rows = plan.few ? plan.few_rows : 0, p.few_stride = plan.few_stride;
     p.few_waves = plan.few_groups * kLineWaves, p.few_least = kFewLeast, p.many_chunk = plan.many_chunk;
     char* space = (char*)workspace;

@@ -155,3 +155,10 @@ def test_workspaces_do_not_grow_with_the_length():
     assert b.ap_attention_workspace(_cache(), batch(1 << 20, 1), 8, 100, 4) == 0     # a window makes them short
     whole = b.make_seq_batch(1, 16384, 16384, 1 << 20, AT, AT, AT, 1 << 16)
     assert b.ap_attention_workspace(_cache(), whole, 8) == 0                         # many rows: enough work without a split
+
+
+def test_scales_beyond_what_scores_are_held_in():
+    """Scores are held in powers of two, so a scale is refused where log2(e) times it is no number of 32 bits."""
+    for scale in (2.4e38, 3e38):
+        _refused(b.AP_ERR_INVALID, b.ap_attention, _cache(), _batch(), _rows(), _rows(), 8, scale, 0, 0, AT, 1 << 40)
+    b.ap_attention(_cache(), _batch(n_tokens=0, max_new=0), _rows(), _rows(), 8, 2.3e38)
