@@ -99,10 +99,13 @@ ap_status ap_kv_read(const ap_kv_cache *cache, const ap_seq_batch *batch, const 
  *     j <= p, j < kv_len, j < max_kv, on a page, and with window > 0 also j > p - window or j < sinks.
  * A row that sees nothing (or only scores of minus infinity) is zero.  Keys and values that a row does not see do not
  * reach it, whatever they hold.  q_heads is a multiple of kv_heads: q head h reads key/value head h / (q_heads / kv_heads).
- * Scores, maxima and sums are in 32 bits; weights are rounded to 16 bits before they meet the values.  Weights are held up to
- * 2^15 times their size, so a row whose sum of values passes 2^112 can overflow to an infinity.  q . k, its parts and scale times
- * it are numbers of 32 bits: where one overflows, the row can be NaN.  Values in 4 bits are used as lo + step * code with at least the 16-bit type's
- * precision.
+ * Scores, maxima and sums are in 32 bits.  Weights are rounded to 16 bits before they meet the values, and summed as rounded: that
+ * moves a row by at most half a step of the type (2^-8 bf16, 2^-11 fp16) of the weighted mean of |v_j - out|, beside the half step of
+ * its own last rounding.  With random rows the two together are 1.3 to 1.4 times the last rounding alone (0.0022 of a row's size
+ * in bf16, 0.00027 in fp16).  Up to 32 rows over 4 bits round a weight times its key's step, against what codes are off the middle one.
+ * Weights are held up to 2^15 times their size, so a row whose sum of values passes 2^112 can overflow to an infinity.  q . k, its
+ * parts and scale times it are numbers of 32 bits: where one overflows, the row can be NaN.  Values in 4 bits are used as
+ * lo + step * code with at least the 16-bit type's precision.
  *   scale     : > 0, and log2(e) times it finite.
  *   workspace : device memory of at least ap_attention_workspace bytes, aligned to 16 bytes (may be NULL where that
  *               is 0), for this call alone until it has run.

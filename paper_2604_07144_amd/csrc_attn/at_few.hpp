@@ -472,11 +472,11 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     x[n][j] = exp2_of(fmaf(x[n][j], unit_of[n], -from));
-                    l[n] += x[n][j];
+                    if constexpr (kCodes) l[n] += x[n][j];
                 }
                 if constexpr (!kCodes) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w[n][j] = pack2<E>(x[n][2 * j], x[n][2 * j + 1]);
+                    for (int j = 0; j < 4; ++j) w[n][j] = pack2<E>(x[n][2 * j], x[n][2 * j + 1]), l[n] = add2<E>(w[n][j], l[n]);
                 }
             }
             if constexpr (kCodes) {

@@ -411,8 +411,8 @@ __global__ __launch_bounds__(kManyThreads, (kManyPerCu<D, kBits>)) void k_attend
 #pragma unroll
                 for (int j = 0; j < 16; j += 2) {
                     const float a = exp2_of(fmaf(sc[t][j], unit, -from)), b = exp2_of(fmaf(sc[t][j + 1], unit, -from));
-                    l += a + b;
                     w[2 * t + j / 8][j % 8 / 2] = pack2<T>(a, b);
+                    l = add2<T>(w[2 * t + j / 8][j % 8 / 2], l);
                 }
             const uint32_t key_in = 4 * half + (lane % 16) / 4, piece_in = ((lane / 16) % 2) * 2 + (lane % 4) / 2, byte_in = (lane % 2) * 8;
             const uint32_t value_at = here(key_in * (2 * D) + value_piece<D>(key_in, piece_in) * 16 + byte_in);

@@ -86,6 +86,13 @@ __device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_
 // The exponent above x > 0: x < 2^e.
 __device__ __forceinline__ int exponent_above(float x) { return (int)(__float_as_uint(x) >> 23) - 126; }
 
+// sum + both halves of a dword of weights, in 32 bits: what rows are divided by is the sum of the weights that meet the values, so
+// that their rounding moves a row only by how values differ (and a row of one value alone is that value).
+template <typename E> __device__ __forceinline__ float add2(uint32_t two, float sum) {
+    if constexpr (std::is_same_v<E, bf16>) return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Vec2<bf16>, two), __builtin_bit_cast(Vec2<bf16>, 0x3F803F80u), sum, false);
+    else return __builtin_amdgcn_fdot2(__builtin_bit_cast(Vec2<fp16>, two), __builtin_bit_cast(Vec2<fp16>, 0x3C003C00u), sum, false);
+}
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126: 0
 
 // Joins the parts of a row, which lie at `at(0)` .. `at(n - 1)`.  Each lane has the (m, l) of a part; then 16 lanes read the

@@ -105,3 +105,35 @@ def test_scales_that_leave_no_score(new, bits):
     r = Replica([200, 333], [new, new], K=1, A=4, bits=bits)
     q = r.made(r.T, r.A, r.d).to(r.dtype)
     check(r.attend(q, 1e-42, 90, 2), *r.expected(q, 1e-42, 90, 2))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("K, A, held, new", [(1, 4, 40, 1), (1, 4, 300, 1), (4, 4, 4000, 1), (1, 4, 700, 6), (1, 24, 700, 1), (1, 4, 300, 100), (1, 4, 5000, 40)])
+def test_equal_values_come_back_as_they_are(K, A, held, new, dtype, d, bits):
+    """All values of a channel alike, under weights that all round the same way: a row is a mean of one value, which is that value.
+
+    The value lies just below a power of two, where half a step is the smallest part of it; weights in 16 bits are taken off it by nearly
+    half a step of theirs at the bottom of their step, twice that part.  32 bits leave 2^-14 of half a step beside that."""
+    r = Replica([held] * 3, [new] * 3, K=K, A=A, d=d, dtype=dtype, bits=bits, page=20)
+    u = torch.finfo(r.dtype).eps / 2
+    value = 2.0 - 2 * u
+    if bits == 16:
+        r.k.zero_()
+        r.k[..., 0] = -1.0
+        for s in range(3):
+            r.k[int(r.table[s, 0]), :, 0, 0] = 0.0          # the first key has the maximum
+        r.v[:] = value
+    else:                                                   # steps of zero: lo alone
+        r.kp.zero_()
+        r.kp[..., 1] = -1.0
+        for s in range(3):
+            r.kp[int(r.table[s, 0]), :, 0, 1] = 0.0
+        r.vp.zero_()
+        r.vp[..., 1::2] = value
+    q = torch.zeros((r.T, A, d), dtype=r.dtype, device="cuda")
+    q[..., 0] = 1.0
+    scale = -float(np.log(0.5 * (1 + u * (1 - 2.0 ** -3))))
+    got = r.attend(q, scale)
+    assert (got.double() == value).all(), (got.double().min().item(), got.double().max().item(), value)
