@@ -137,3 +137,29 @@ def test_equal_values_come_back_as_they_are(K, A, held, new, dtype, d, bits):
     scale = -float(np.log(0.5 * (1 + u * (1 - 2.0 ** -3))))
     got = r.attend(q, scale)
     assert (got.double() == value).all(), (got.double().min().item(), got.double().max().item(), value)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("held, new", [(150, 60), (300, 300), (3000, 130)])
+@pytest.mark.parametrize("size", [2.0 ** -6, 2.0 ** -7, 2.0 ** -9])
+def test_small_groups_keep_eleven_bits(size, held, new, d):
+    """Many rows over 4 bits whose groups are small as a whole: neighbouring codes, which bf16 would round apart or together, still
+    give their own scores, and values of the same size.
+
+    Keys and values are rounded to 11 bits (u = 2^-11 of each) and lose at most 17 * 2^-25 by the range of fp16; a key's error moves a
+    score by that much of the sum of |q| scale, and a weight by twice that."""
+    r = Replica([held], [new], K=1, A=4, d=d, bits=4)
+    odd = torch.from_numpy(r.rng.integers(0, 2, (r.n_pages, 1, r.page, 1), dtype=np.uint8)).cuda()
+    r.k[:] = 0x11 + 0x22 * odd                              # codes 1 and 3, half-way between numbers of bf16: to 0 and to 4
+    r.v[:] = 0xFF * odd
+    r.kp[..., 0::2], r.kp[..., 1::2] = size / 256, size
+    r.vp[..., 0::2], r.vp[..., 1::2] = size / 8, -size * 15 / 16
+    q = torch.ones((r.T, r.A, d), dtype=r.dtype, device="cuda")
+    scale, u, lost = 64 / (d * size), 2.0 ** -11, 17 * 2.0 ** -25
+
+    def own(mean, seen, live, k, v):
+        moved = ((d + 4) * 2.0 ** -24 + u) * live + scale * d * lost
+        return mean * (2 * u * (1 + u) + 2 * moved * (1 + moved)) + lost + seen * 2.0 ** -31 * size
+
+    tokens = [0, new // 3, new - 1]
+    check(r.attend(q, scale)[tokens], *_rows(r, q, scale, tokens, own))
