@@ -71,7 +71,8 @@ __device__ __forceinline__ float sum_halves(float x) {
 
 // 16 bytes of each lane from memory to LDS, to `to` + 16 * lane.  The data passes no register, so that nothing here is in
 // flight that the compiler could take for there; wait_loads() has to come between it and the barrier after which it is read.
-// (m0, which the compiler keeps nothing in across statements, says where in LDS.)
+// (m0 says where in LDS: a reserved register, in which the compiler keeps nothing and which it takes in no list of what a statement
+// changes.)
 __device__ __forceinline__ void load_to_lds(const char* from, const void* to) {
     const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)to);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(at), "v"(from) : "memory");
