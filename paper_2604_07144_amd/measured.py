@@ -109,11 +109,28 @@ def _roofline_attention_us(model, gpu, batch, n, c):
     return flops / np.minimum(flops / nbytes * gpu["hbm_bytes_per_s"], gpu["flops"]) * 1e6
 
 
+def _times(grid, us, longest, what):
+    """The lengths and times of a measurement as arrays, or ValueError where they say nothing of lengths up to ``longest``."""
+    grid, us = np.asarray(grid, np.float64), np.asarray(us, np.float64)
+    if grid.ndim != 1 or len(grid) == 0 or grid.shape != us.shape or not (np.diff(grid) > 0).all() or not grid[0] > 0:
+        raise ValueError(f"{what}: lengths have to ascend from above 0, with a time for each")
+    if not (np.isfinite(us).all() and (us >= 0).all()):
+        raise ValueError(f"{what}: times have to be numbers that are not negative")
+    if grid[-1] < longest:
+        raise ValueError(f"{what}: measured up to {grid[-1]:g} tokens, and {longest} are needed")
+    return grid, us
+
+
 def request_tables(model, gpu, batch: int, prompt_len, out_len, contexts, decode_us, prompts, prefill_us):
     """``prefill_us`` and ``tpot_us`` (uint32 [1][R], for ``ap_costtable_set``) of requests on a replica of one GPU: the roofline's
-    times with its attention term replaced by the measured ones, which are interpolated between the lengths they were taken at."""
+    times with its attention term replaced by the measured ones, which are interpolated between the lengths they were taken at.
+
+    Lengths ascend and reach the longest prompt (``prompts``) and the longest context of a decode step (``contexts``), otherwise
+    ValueError; what is shorter than the first length takes the first time."""
     prompt, out = np.asarray(prompt_len, np.int64), np.asarray(out_len, np.int64)
     longest = int((prompt + out).max())
+    contexts, decode_us = _times(contexts, decode_us, longest - 1, "decode steps")
+    prompts, prefill_us = _times(prompts, prefill_us, int(prompt.max()), "prefills")
     group = np.array([(0, 0, 1, batch)], dtype=binding.GROUP_DTYPE)
     pre_ns, prefix_ns, _, _ = binding.ap_roofline_tables(np.array([model], binding.MODEL_DTYPE), np.array([gpu], binding.GPU_DTYPE), group, longest)
     length = np.arange(1, longest + 1, dtype=np.float64)
