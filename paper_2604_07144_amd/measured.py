@@ -121,9 +121,25 @@ def _times(grid, us, longest, what):
     return grid, us
 
 
+def _between(length, grid, us):
+    """Times at ``length``: between two lengths of the grid the mean of the parabolas through both and either neighbour, which is exact
+    where times go as a + b n + c n^2, and never outside of the two's times; the first time below the grid."""
+    if len(grid) == 1:
+        return np.full(len(length), us[0])
+    at = np.clip(length, grid[0], grid[-1])
+    i = np.clip(np.searchsorted(grid, at, "right") - 1, 0, len(grid) - 2)
+    slope = np.diff(us) / np.diff(grid)
+    bend = np.zeros_like(slope)
+    if len(grid) > 2:
+        of_three = np.diff(slope) / (grid[2:] - grid[:-2])
+        bend = np.concatenate([of_three[:1], (of_three[1:] + of_three[:-1]) / 2, of_three[-1:]])
+    y = us[i] + (at - grid[i]) * (slope[i] + bend[i] * (at - grid[i + 1]))
+    return np.clip(y, np.minimum(us[i], us[i + 1]), np.maximum(us[i], us[i + 1]))
+
+
 def request_tables(model, gpu, batch: int, prompt_len, out_len, contexts, decode_us, prompts, prefill_us):
     """``prefill_us`` and ``tpot_us`` (uint32 [1][R], for ``ap_costtable_set``) of requests on a replica of one GPU: the roofline's
-    times with its attention term replaced by the measured ones, which are interpolated between the lengths they were taken at.
+    times with its attention term replaced by the measured ones, interpolated by parabolas between the lengths they were taken at.
 
     Lengths ascend and reach the longest prompt (``prompts``) and the longest context of a decode step (``contexts``), otherwise
     ValueError; what is shorter than the first length takes the first time."""
@@ -135,7 +151,7 @@ def request_tables(model, gpu, batch: int, prompt_len, out_len, contexts, decode
     pre_ns, prefix_ns, _, _ = binding.ap_roofline_tables(np.array([model], binding.MODEL_DTYPE), np.array([gpu], binding.GPU_DTYPE), group, longest)
     length = np.arange(1, longest + 1, dtype=np.float64)
     layers = float(model["layers"])
-    change = lambda grid, us, n: layers * (np.interp(length, grid, us) - _roofline_attention_us(model, gpu, batch, n, length))   # noqa: E731
+    change = lambda grid, us, n: layers * (_between(length, grid, us) - _roofline_attention_us(model, gpu, batch, n, length))   # noqa: E731
     pre = np.asarray(pre_ns, np.float64).reshape(-1)[1:longest + 1] / 1e3 + change(prompts, prefill_us, length)
     step = np.diff(np.asarray(prefix_ns, np.float64).reshape(-1))[1:longest + 1] / 1e3 + change(contexts, decode_us, 1.0)
     upto = np.concatenate([[0.0], np.cumsum(step)])          # of contexts 1 .. k
