@@ -12,14 +12,16 @@ import torch
 
 from . import binding
 
+CHIP_CACHE = 256 << 20                  # bytes: the largest of the card's caches
 DTYPES = {"bf16": (torch.bfloat16, binding.AP_BF16), "fp16": (torch.float16, binding.AP_FP16)}
 
 
 class ReplicaLayer:
     """One layer's cache of a replica: ``batch`` slots of up to ``max_len`` tokens in shuffled pages, and a step over them.
 
-    ``heads``, ``kv_heads`` and ``head_dim`` are the layer's; ``bits`` is what the cache is held in (16 or 4).  Caches of
-    ``copies`` layers take turns, as a model's layers do, so that a step does not find its own in the caches of the chip."""
+    ``heads``, ``kv_heads`` and ``head_dim`` are the layer's; ``bits`` is what the cache is held in (16 or 4).  There are caches of
+    ``copies`` layers.  Steps of fewer than ``max_len`` tokens take turns at the pages that a slot has, then at the caches, so that each of
+    them comes back to its pages only after all the others, as a layer of a served model does."""
 
     def __init__(self, batch: int, max_len: int, heads: int, kv_heads: int, head_dim: int, *, dtype: str = "bf16", bits: int = 16,
                  page: int = 16, copies: int = 1, window: int = 0, sinks: int = 0, device: str = "cuda", seed: int = 0):
@@ -44,10 +46,11 @@ class ReplicaLayer:
         angle = torch.arange(max_len, device=device, dtype=torch.float64)[:, None] * \
             10000.0 ** (-torch.arange(0, head_dim, 2, device=device, dtype=torch.float64) / head_dim)
         self.turn = torch.stack([angle.cos(), angle.sin()], -1).float()
-        self.gen, self.at = gen, 0
+        self.gen = gen
 
     def plan(self, held: int, new: int) -> dict:
-        """Memory and descriptions of a step in which every slot holds ``held`` tokens, ``new`` of them new."""
+        """Memory and descriptions of steps in which every slot holds ``held`` tokens, ``new`` of them new: ``turns`` of them, a cache and
+        its pages each.  The first one's pages are the first of each slot."""
         if not 1 <= new <= held <= self.max_len:
             raise ValueError(f"a step of {new} new tokens of {held} in slots of {self.max_len}")
         b, T, made = self.batch, self.batch * new, lambda h: torch.randn((self.batch * new, h, self.head_dim), generator=self.gen, device=self.device).to(self.torch_dtype)
@@ -55,36 +58,41 @@ class ReplicaLayer:
                  q=made(self.heads), k=made(self.kv_heads), v=made(self.kv_heads))
         p["turned"], p["out"] = torch.empty_like(p["q"]), torch.empty_like(p["q"])
         p["rows"] = {f: binding.make_rows(p[f].data_ptr(), p[f].shape[1], self.head_dim) for f in ("q", "k", "v", "turned", "out")}
-        p["batch"] = binding.make_seq_batch(b, T, new, held, p["first"].data_ptr(), p["held"].data_ptr(), self.table.data_ptr(), self.table.shape[1])
-        p["caches"] = [binding.make_kv_cache(self.dtype, self.bits, self.n_pages, self.page, self.kv_heads, self.head_dim, *(x.data_ptr() for x in c))
-                       for c in self.caches]
+        width, pages = self.table.shape[1], -(-held // self.page)
+        batches = [binding.make_seq_batch(b, T, new, held, p["first"].data_ptr(), p["held"].data_ptr(), self.table.data_ptr() + 4 * at, pages, width)
+                   for at in range(0, width - pages + 1, pages)]
+        caches = [binding.make_kv_cache(self.dtype, self.bits, self.n_pages, self.page, self.kv_heads, self.head_dim, *(x.data_ptr() for x in c))
+                  for c in self.caches]
+        p["at"], p["turns"] = 0, [(c, x) for x in batches for c in caches]
         p["rotation"] = binding.make_rotation(self.turn.data_ptr(), self.max_len, self.head_dim)
-        p["space"] = torch.empty(max(16, binding.ap_attention_workspace(p["caches"][0], p["batch"], self.heads, self.window, self.sinks)),
+        p["space"] = torch.empty(max(16, binding.ap_attention_workspace(caches[0], batches[0], self.heads, self.window, self.sinks)),
                                  dtype=torch.uint8, device=self.device)
         return p
 
     def step(self, p: dict) -> torch.Tensor:
         """The new tokens into the cache, turned, and their attention over it: [token][head][channel]."""
-        cache, rows, stream = p["caches"][self.at], p["rows"], torch.cuda.current_stream().cuda_stream
-        self.at = (self.at + 1) % len(self.caches)
-        binding.ap_kv_append(cache, p["batch"], rows["k"], rows["v"], p["rotation"], rows["q"], rows["turned"], self.heads, stream)
-        binding.ap_attention(cache, p["batch"], rows["turned"], rows["out"], self.heads, self.scale, self.window, self.sinks,
+        (cache, batch), rows, stream = p["turns"][p["at"]], p["rows"], torch.cuda.current_stream().cuda_stream
+        p["at"] = (p["at"] + 1) % len(p["turns"])
+        binding.ap_kv_append(cache, batch, rows["k"], rows["v"], p["rotation"], rows["q"], rows["turned"], self.heads, stream)
+        binding.ap_attention(cache, batch, rows["turned"], rows["out"], self.heads, self.scale, self.window, self.sinks,
                              p["space"].data_ptr(), p["space"].numel(), stream)
         return p["out"]
 
     def time_us(self, held: int, new: int, repeats: int = 20) -> float:
         """Microseconds of a step among others: the median of five timings of ``repeats`` steps each.  The steps are recorded into a graph,
-        so that the device's time is taken and not that of the host's calls."""
+        so that the device's time is taken and not that of the host's calls; before each timing the caches of the chip are filled with
+        other memory."""
         p = self.plan(held, new)
         self.step(p)
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             for _ in range(repeats):
                 self.step(p)
-        times = []
+        other, times = torch.zeros(2 * CHIP_CACHE // 4, dtype=torch.int32, device=self.device), []
+        graph.replay()
         for _ in range(5):
             a, z = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-            graph.replay()                                  # keeps the device busy until what is timed has been sent
+            other.sum()                                     # also keeps the device busy until what is timed has been sent
             a.record()
             graph.replay()
             z.record()
@@ -101,7 +109,7 @@ def layer_times(model, batch: int, contexts, prompts, *, dtype: str = "bf16", bi
     longest = max(*contexts, *prompts)
     size = 2 * batch * (-(-longest // page) * page) * kv_heads * (2 * d if bits == 16 else d // 2 + d // 16)
     layer = ReplicaLayer(batch, longest, heads, kv_heads, d, dtype=dtype, bits=bits, page=page, window=window, sinks=sinks,
-                         copies=max(1, min(int(model["layers"]), (1 << 30) // size)))
+                         copies=-(-4 * CHIP_CACHE // size))      # steps come back to their pages after at least half of all
     return (np.array([layer.time_us(int(c), 1, repeats) for c in contexts]),
             np.array([layer.time_us(int(s), int(s), max(2, repeats // 4)) for s in prompts]))
 
