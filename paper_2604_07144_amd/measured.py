@@ -27,7 +27,8 @@ class ReplicaLayer:
                  page: int = 16, copies: int = 1, window: int = 0, sinks: int = 0, device: str = "cuda", seed: int = 0):
         self.batch, self.max_len, self.heads, self.kv_heads, self.head_dim = batch, max_len, heads, kv_heads, head_dim
         self.torch_dtype, self.dtype = DTYPES[dtype]
-        self.bits, self.page, self.window, self.sinks, self.device = bits, page, window, sinks, device
+        self.bits, self.page, self.window, self.sinks = bits, page, window, sinks
+        self.device = device = torch.empty(0, device=device).device    # with its number
         self.scale = head_dim ** -0.5
         gen = torch.Generator(device=device)
         gen.manual_seed(seed)
@@ -71,33 +72,36 @@ class ReplicaLayer:
 
     def step(self, p: dict) -> torch.Tensor:
         """The new tokens into the cache, turned, and their attention over it: [token][head][channel]."""
-        (cache, batch), rows, stream = p["turns"][p["at"]], p["rows"], torch.cuda.current_stream().cuda_stream
+        (cache, batch), rows = p["turns"][p["at"]], p["rows"]
         p["at"] = (p["at"] + 1) % len(p["turns"])
-        binding.ap_kv_append(cache, batch, rows["k"], rows["v"], p["rotation"], rows["q"], rows["turned"], self.heads, stream)
-        binding.ap_attention(cache, batch, rows["turned"], rows["out"], self.heads, self.scale, self.window, self.sinks,
-                             p["space"].data_ptr(), p["space"].numel(), stream)
+        with torch.cuda.device(self.device):                # kernels go to the device that is the present one
+            stream = torch.cuda.current_stream().cuda_stream
+            binding.ap_kv_append(cache, batch, rows["k"], rows["v"], p["rotation"], rows["q"], rows["turned"], self.heads, stream)
+            binding.ap_attention(cache, batch, rows["turned"], rows["out"], self.heads, self.scale, self.window, self.sinks,
+                                 p["space"].data_ptr(), p["space"].numel(), stream)
         return p["out"]
 
     def time_us(self, held: int, new: int, repeats: int = 20) -> float:
         """Microseconds of a step among others: the median of five timings of ``repeats`` steps each.  The steps are recorded into a graph,
         so that the device's time is taken and not that of the host's calls; before each timing the caches of the chip are filled with
         other memory."""
-        p = self.plan(held, new)
-        self.step(p)
-        graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
-            for _ in range(repeats):
-                self.step(p)
-        other, times = torch.zeros(2 * CHIP_CACHE // 4, dtype=torch.int32, device=self.device), []
-        graph.replay()
-        for _ in range(5):
-            a, z = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-            other.sum()                                     # also keeps the device busy until what is timed has been sent
-            a.record()
+        with torch.cuda.device(self.device):
+            p = self.plan(held, new)
+            self.step(p)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                for _ in range(repeats):
+                    self.step(p)
+            other, times = torch.zeros(2 * CHIP_CACHE // 4, dtype=torch.int32, device=self.device), []
             graph.replay()
-            z.record()
-            z.synchronize()
-            times.append(a.elapsed_time(z) * 1e3 / repeats)
+            for _ in range(5):
+                a, z = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+                other.sum()                                     # also keeps the device busy until what is timed has been sent
+                a.record()
+                graph.replay()
+                z.record()
+                z.synchronize()
+                times.append(a.elapsed_time(z) * 1e3 / repeats)
         return float(np.median(times))
 
 

@@ -82,3 +82,28 @@ def test_every_turn_is_a_step_over_its_own_pages(bits):
     if bits == 16:
         rows = cache[1][layer.table[:, 7 + 99 // 16].long(), :, 99 % 16]
         assert torch.equal(rows, p["v"].view(3, 5, 2, 128)[:, 4])
+
+
+def test_calls_are_made_with_the_layers_device_as_the_present_one(monkeypatch):
+    """Kernels go to the present device, so a layer of another one makes it that for its calls."""
+    layer, active, devices = measured.ReplicaLayer(1, 64, 2, 2, 64, device="cuda:0"), [], []
+    real, append, attention = torch.cuda.device, binding.ap_kv_append, binding.ap_attention
+
+    class Guard(real):
+        def __enter__(self):
+            active.append(self.idx)
+            return super().__enter__()
+
+        def __exit__(self, *args):
+            active.pop()
+            return super().__exit__(*args)
+
+    def logged(call):
+        return lambda *args: (devices.append(active[-1] if active else None), call(*args))
+
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(binding, "ap_kv_append", logged(append))
+    monkeypatch.setattr(binding, "ap_attention", logged(attention))
+    layer.step(layer.plan(20, 1))
+    layer.time_us(20, 1, repeats=2)
+    assert len(devices) >= 4 and set(devices) == {0} and not active
