@@ -7,6 +7,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 from oracle import attention as orc                        # noqa: E402
+from paper_2604_07144_amd import binding as b              # noqa: E402
 from tests.attn_harness import Replica, check              # noqa: E402
 
 
@@ -58,7 +59,7 @@ def test_many_small_weights_in_fp16(held, K, A, new, d):
     check(r.attend(q, scale)[tokens], want, tol)
 
 
-def _code_rows(r, q, scale, tokens, window=0, sinks=0):
+def _code_error(r, q, scale):
     """Bounds for few rows over 4 bits, where codes are multiplied as they are and nothing but each weight, times its key's step, is rounded
     to 16 bits.
 
@@ -78,7 +79,11 @@ def _code_rows(r, q, scale, tokens, window=0, sinks=0):
         lost = seen * 2.0 ** -31 * step if r.dtype == torch.float16 else 0.0
         return 8 * step * u + mean * moved * (1 + moved) + (seen / 16 + 40) * 2.0 ** -24 * (15 * step + lo) + lost + (2.0 ** -25 if r.dtype == torch.float16 else 0.0)
 
-    return _rows(r, q, scale, tokens, own, window, sinks)
+    return own
+
+
+def _code_rows(r, q, scale, tokens, window=0, sinks=0):
+    return _rows(r, q, scale, tokens, _code_error(r, q, scale), window, sinks)
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -163,3 +168,31 @@ def test_small_groups_keep_eleven_bits(size, held, new, d):
 
     tokens = [0, new // 3, new - 1]
     check(r.attend(q, scale)[tokens], *_rows(r, q, scale, tokens, own))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d, A, new, longest", [(64, 16, 1, 32640), (64, 16, 1, 32641), (64, 40, 3, 32641), (128, 160, 1, 16256), (128, 160, 1, 16257), (128, 40, 5, 16257)])
+def test_lines_of_4_bits_on_either_side_of_twice_the_wavefronts(d, A, new, longest, dtype):
+    """The lengths from which the kernel of few rows over 4 bits puts twice as many wavefronts on a SIMD (64 channels up to 16 rows, 128
+    channels from 17 to 32), the last ones below, and what stands in the workspace then."""
+    K, held = 8, np.array([longest, 5, longest // 2, 3000])
+    r = Replica(held, np.minimum(held, new), K=K, A=A, d=d, dtype=dtype, bits=4, page=64, wide=2)
+    cache, batch = r.describe()
+    above, below = (b.ap_attention_workspace(cache, b.make_seq_batch(4, r.T, new, n, 64, 64, 64, r.width), A) for n in (longest + 64, longest - 64))
+    need = b.ap_attention_workspace(cache, batch, A)
+    assert above > 1.9 * below and need == (above if longest % 32 else below)
+    q = (0.5 * r.made(r.T, A, d)).to(r.dtype)
+    got, scale = r.attend(q, d ** -0.5).double().cpu().numpy(), d ** -0.5
+    own, where, qq = _code_error(r, q, scale), orc.new_tokens(r.first, r.held, r.T), q.double().cpu().numpy()
+    for s, head in ((0, 0), (0, K - 1), (1, 3), (2, 5), (3, K - 1)):
+        j = torch.arange(int(held[s]), device="cuda")
+        page, slot = torch.from_numpy(r.table[s].astype(np.int64)).cuda()[j // 64], j % 64
+        rows = []
+        for codes, pairs in ((r.k, r.kp), (r.v, r.vp)):
+            c, two = codes[page, head, slot].cpu().numpy(), pairs[page, head, slot].double().cpu().numpy()
+            rows.append(np.repeat(two[:, 1::2], 64, 1) + np.repeat(two[:, 0::2], 64, 1) * np.stack([c & 15, c >> 4], -1).reshape(len(c), d))
+        for t in (int(r.first[s]), int(r.first[s + 1]) - 1):
+            for h in (head * (A // K), (head + 1) * (A // K) - 1):
+                o, mean, seen = orc.attention(qq[t, h], *rows, where[t, 1], np.ones(len(j), bool), scale, 0, 0)
+                tol = own(mean, seen, None, *rows) + torch.finfo(r.dtype).eps / 2 * np.abs(o) * (1 + 2.0 ** -7) + 1e-30
+                assert (np.abs(got[t, h] - o) <= tol).all(), (s, t, h, np.max(np.abs(got[t, h] - o) / tol))
