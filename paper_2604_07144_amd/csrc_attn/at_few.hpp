@@ -22,10 +22,10 @@
 //    64 channels; for values each weight is multiplied by the key's step before its one rounding, and lo is summed apart
 //    in 32 bits.  So neither keys nor values are rounded at all.
 //
-// Measured, one token, 128 channels, bf16: 64 sequences of 4096 to 8192, 32 heads of their own 6.0 TB/s in 16 bits and 5.3 in 4;
-// with 32 heads on 8 5.7 and 4.5.  Shorter batches pay 5 us for the launch that joins, and 4 bits are bound by instructions
-// there: about 380 a tile of 32 keys, 55 % of what the SIMDs give out, so 64 slots with bimodal lengths take 36 to 38 us
-// (3.1 TB/s) where 16 bits take 88 (4.6).
+// Measured, one token, 128 channels, bf16: 64 sequences of 4096 to 8192, 32 heads of their own 6.0 TB/s in 16 bits and 5.2 in 4;
+// with 32 heads on 8 5.6 and 4.7.  Shorter batches pay 5 us for the launch that joins, and 4 bits are bound by instructions
+// there: about 380 a tile of 32 keys, 45 % of what the SIMDs give out, so 64 slots with bimodal lengths take 39 us
+// (2.9 TB/s) where 16 bits take 88 (4.6).
 #ifndef AT_FEW_HPP
 #define AT_FEW_HPP
 
@@ -80,7 +80,8 @@ struct FewSeq {
 template <uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
 constexpr uint32_t kFewWaves = kTeam && !(D == 128 && kBits == 16 && kTiles == 2) ? 8 : 4;
 
-// Variants of the line (4 bits) that run with twice the wavefronts on a SIMD where each still has a good share of the line.
+// Variants of the line (4 bits) that run with twice the wavefronts on a SIMD where each still has a good share of the line.  (128
+// channels have 15 of their 256 registers in scratch memory then.)
 template <uint32_t D, uint32_t kBits, uint32_t kTiles, bool kTeam>
 constexpr bool kFewDoubles = kBits == 4 && !kTeam && (D == 64 ? kTiles == 1 : kTiles == 2);
 // Wavefronts that registers leave room for on a SIMD.
@@ -98,7 +99,7 @@ __global__ __launch_bounds__((kFewWaves<D, kBits, kTiles, kTeam> * kLanes), (kFe
     constexpr uint32_t kLaneRows = kRowBytes / 16;          // lanes that read a row
     constexpr uint32_t kRowsAtOnce = kLanes / kLaneRows, kLoads = kFewKeys / kRowsAtOnce;
     constexpr uint32_t kPairFloats = 2 * kGroups;           // (step, lo) of a key
-    // A maximum is only raised when a score passes it by 2^this; in 4 bits and fp16 that comes off the weights' range.
+    // A maximum is only raised when a score, in powers of two, passes it by this; in 4 bits and fp16 that comes off the weights' range.
     constexpr float kFewHeadroom = kCodes && std::is_same_v<E, fp16> ? 4.0f : 8.0f;
     constexpr float kUp = kCodes ? 0.0f : kWeightUp<E>;     // (codes have their own, with the step)
     constexpr int kWeightExponent = std::is_same_v<E, fp16> ? 10 : 100;

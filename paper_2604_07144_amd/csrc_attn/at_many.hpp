@@ -7,13 +7,13 @@
 // wavefront has 32 rows as columns, its queries and results stay in registers, the weights go from the first product's
 // result registers to the second's operands without moving, and the maximum of a row is over one lane's registers and one
 // exchange between the halves of the wavefront.  The maximum that weights are taken against is only raised when a score
-// passes it by 2^8, which 32-bit sums and 16-bit weights both have room for.  Two wavefronts of a SIMD take turns at the
+// passes it by 8 (a weight would by 2^8), which 32-bit sums and 16-bit weights both have room for.  Two wavefronts of a SIMD take turns at the
 // matrix units and the exponentials.  The next 64 keys and values are on their way to the other of two LDS buffers while
 // the present ones are worked on: in 16 bits without passing through registers, in 4 bits decoded on the way.
 //
-// Measured, 32 heads on 8, 128 channels, bf16: the last 2048 tokens of 32768 at 940 to 970 TFLOP/s (a large matrix product of the
+// Measured, 32 heads on 8, 128 channels, bf16: the last 2048 tokens of 32768 at 935 to 960 TFLOP/s (a large matrix product of the
 // library 1200), whole prompts of 8192 840, of 1024 550, of 512 380: a workgroup's first tile waits for four trips to memory.
-// In 4 bits 150 instructions a tile and wavefront of decoding are added, and 770 TFLOP/s are reached.
+// In 4 bits 150 instructions a tile and wavefront of decoding are added, and 740 TFLOP/s are reached.
 #ifndef AT_MANY_HPP
 #define AT_MANY_HPP
 
