@@ -113,7 +113,7 @@ def layer_times(model, batch: int, contexts, prompts, *, dtype: str = "bf16", bi
     longest = max(*contexts, *prompts)
     size = 2 * batch * (-(-longest // page) * page) * kv_heads * (2 * d if bits == 16 else d // 2 + d // 16)
     layer = ReplicaLayer(batch, longest, heads, kv_heads, d, dtype=dtype, bits=bits, page=page, window=window, sinks=sinks,
-                         copies=-(-4 * CHIP_CACHE // size))      # steps come back to their pages after at least half of all
+                         copies=max(1, min(repeats, -(-4 * CHIP_CACHE // size))))   # as many turns as steps, or half of these bytes between two visits
     return (np.array([layer.time_us(int(c), 1, repeats) for c in contexts]),
             np.array([layer.time_us(int(s), int(s), max(2, repeats // 4)) for s in prompts]))
 

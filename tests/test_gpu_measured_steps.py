@@ -107,3 +107,25 @@ def test_calls_are_made_with_the_layers_device_as_the_present_one(monkeypatch):
     layer.step(layer.plan(20, 1))
     layer.time_us(20, 1, repeats=2)
     assert len(devices) >= 4 and set(devices) == {0} and not active
+
+
+@pytest.mark.parametrize("batch, longest", [(1, 16), (8, 64), (64, 300)])
+def test_short_models_do_not_make_more_caches_than_steps(batch, longest, monkeypatch):
+    """Where a cache is small, as many turns as there are steps in a timing do: the chip's caches hold other memory when it begins."""
+    model, made, steps = np.array((4, 256, 2048, 1000, 4, 1, 16), dtype=binding.MODEL_DTYPE), [], []
+    init, attention = measured.ReplicaLayer.__init__, binding.ap_attention
+
+    def logged(layer, *args, **kw):
+        init(layer, *args, **kw)
+        made.append(layer)
+
+    def call(cache, batch, *args):
+        steps.append((cache.k, batch.page_table))
+        attention(cache, batch, *args)
+
+    monkeypatch.setattr(measured.ReplicaLayer, "__init__", logged)
+    monkeypatch.setattr(binding, "ap_attention", call)
+    decode_us, prefill_us = measured.layer_times(model, batch, [longest], [longest], repeats=12)
+    assert decode_us[0] > 0 and prefill_us[0] > 0 and 1 <= len(made[0].caches) <= 12
+    recorded = steps[1:13]                                  # after the first step, the decode steps of the graph
+    assert len(set(recorded)) == 12
