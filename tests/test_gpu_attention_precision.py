@@ -196,3 +196,21 @@ def test_lines_of_4_bits_on_either_side_of_twice_the_wavefronts(d, A, new, longe
                 o, mean, seen = orc.attention(qq[t, h], *rows, where[t, 1], np.ones(len(j), bool), scale, 0, 0)
                 tol = own(mean, seen, None, *rows) + torch.finfo(r.dtype).eps / 2 * np.abs(o) * (1 + 2.0 ** -7) + 1e-30
                 assert (np.abs(got[t, h] - o) <= tol).all(), (s, t, h, np.max(np.abs(got[t, h] - o) / tol))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("held", [200, 3000])
+def test_queries_of_few_rows_that_are_not_numbers(held, dtype, bits):
+    """A NaN or an infinity in a query row stays in it, beside rows of any size and of zeros."""
+    r = Replica([held] * 3, [2] * 3, K=1, A=4, d=128, dtype=dtype, bits=bits)
+    q = r.made(r.T, r.A, r.d).to(r.dtype)
+    q[1, 2] = 0.0
+    q[4, 1] *= 2.0 ** -12
+    clean, tol = r.expected(q, 0.1)
+    q[0, 1, 7], q[3, 0, 64], q[5, 3, 127] = float("nan"), float("inf"), float("-inf")
+    got = r.attend(q, 0.1)
+    assert torch.isnan(got[0, 1].float()).all()
+    rest = np.ones((r.T, r.A), dtype=bool)
+    rest[0, 1] = rest[3, 0] = rest[5, 3] = False
+    check(got[torch.from_numpy(rest).cuda()], clean[rest], tol[rest])
