@@ -1,5 +1,5 @@
 """ctypes binding of ``libautopoiesis_eval.so``: the same names as the C ABI
-(``include/autopoiesis_eval.h``, ``include/autopoiesis_attn.h``), argument marshalling only.  Every step of the
+(``include/autopoiesis_eval.h``, ``include/autopoiesis_attn.h``, ``include/autopoiesis_linear.h``), argument marshalling only.  Every step of the
 evaluation runs in the library's HIP kernels; PyTorch is used by callers for device
 memory and streams.  There is no fallback: a missing library raises at load time.
 """
@@ -62,6 +62,23 @@ class ApRows(C.Structure):
 
 class ApRotation(C.Structure):
     _fields_ = [("table", C.c_void_p), ("n_positions", C.c_uint32), ("rot_dim", C.c_uint32), ("neighbours", C.c_uint32)]
+
+
+AP_FP32 = 2
+AP_SILU, AP_GELU = 0, 1
+
+
+class ApWeights(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "group", "n_out", "n_in")] + [(n, C.c_void_p) for n in ("codes", "pairs")] + \
+               [(n, C.c_int64) for n in ("code_stride", "pair_stride")]
+
+
+class ApVectors(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64)]
+
+
+class ApLogits(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "n_rows", "vocab")] + [("data", C.c_void_p), ("stride", C.c_int64)]
 
 
 class ApError(RuntimeError):
@@ -137,6 +154,15 @@ def lib() -> C.CDLL:
         L.ap_attention_workspace.restype = C.c_int
         L.ap_attention.argtypes = [cache, batch, rows, rows, C.c_uint32, C.c_float, C.c_uint32, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p]
         L.ap_attention.restype = C.c_int
+        weights, vectors, logits, size = C.POINTER(ApWeights), C.POINTER(ApVectors), C.POINTER(ApLogits), C.POINTER(C.c_uint64)
+        for name, args in (("ap_weights_pack", [weights, vectors, C.c_void_p]), ("ap_weights_read", [weights, vectors, C.c_void_p]),
+                           ("ap_linear_workspace", [weights, C.c_uint32, size]),
+                           ("ap_linear", [weights, vectors, vectors, vectors, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p]),
+                           ("ap_gated_workspace", [weights, weights, C.c_uint32, size]),
+                           ("ap_gated", [weights, weights, vectors, vectors, C.c_uint32, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p]),
+                           ("ap_logprobs_workspace", [logits, C.c_uint32, size]),
+                           ("ap_logprobs", [logits, C.c_void_p, C.c_float, C.c_uint32] + [C.c_void_p] * 5 + [C.c_uint64, C.c_void_p])):
+            getattr(L, name).argtypes, getattr(L, name).restype = args, C.c_int
         _lib = L
     return _lib
 
@@ -395,3 +421,70 @@ def ap_attention_workspace(cache: ApKvCache, batch: ApSeqBatch, q_heads: int, wi
 def ap_attention(cache: ApKvCache, batch: ApSeqBatch, q: ApRows, out: ApRows, q_heads: int, scale: float, window: int = 0, sinks: int = 0,
                  workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
     _check(lib().ap_attention(cache, batch, q, out, q_heads, scale, window, sinks, workspace_ptr, workspace_bytes, stream), "ap_attention")
+
+
+def make_weights(dtype: int, group: int, n_out: int, n_in: int, codes_ptr: int, pairs_ptr: int, code_stride: int | None = None,
+                 pair_stride: int | None = None) -> ApWeights:
+    """Describes weights [n_out][n_in] in 4 bits; strides in bytes where rows (``weight_row_bytes``) do not follow one another."""
+    codes, pairs = weight_row_bytes(group, n_in)
+    return ApWeights(dtype, group, n_out, n_in, codes_ptr, pairs_ptr, codes if code_stride is None else code_stride,
+                     pairs if pair_stride is None else pair_stride)
+
+
+def weight_row_bytes(group: int, n_in: int) -> tuple[int, int]:
+    """Bytes of a row's codes and of its pairs."""
+    blocks = -(-n_in // 128)
+    return 64 * blocks, 4 * blocks * (128 // group)
+
+
+def make_vectors(ptr: int, n: int, stride: int | None = None) -> ApVectors:
+    """Rows [token][n] of 2-byte values; the stride in bytes where they are not contiguous."""
+    return ApVectors(ptr, 2 * n if stride is None else stride)
+
+
+def make_logits(dtype: int, n_rows: int, vocab: int, ptr: int, stride: int | None = None) -> ApLogits:
+    return ApLogits(dtype, n_rows, vocab, ptr, vocab * (4 if dtype == AP_FP32 else 2) if stride is None else stride)
+
+
+def ap_weights_pack(weights: ApWeights, values: ApVectors, stream: int = 0) -> None:
+    _check(lib().ap_weights_pack(weights, values, stream), "ap_weights_pack")
+
+
+def ap_weights_read(weights: ApWeights, values: ApVectors, stream: int = 0) -> None:
+    _check(lib().ap_weights_read(weights, values, stream), "ap_weights_read")
+
+
+def ap_linear_workspace(weights: ApWeights, n_tokens: int) -> int:
+    """Bytes of device memory that ap_linear needs for so many tokens."""
+    need = C.c_uint64()
+    _check(lib().ap_linear_workspace(weights, n_tokens, need), "ap_linear_workspace")
+    return need.value
+
+
+def ap_linear(weights: ApWeights, x: ApVectors, y: ApVectors, n_tokens: int, add: ApVectors | None = None, workspace_ptr: int = 0,
+              workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().ap_linear(weights, x, add, y, n_tokens, workspace_ptr, workspace_bytes, stream), "ap_linear")
+
+
+def ap_gated_workspace(gate: ApWeights, up: ApWeights, n_tokens: int) -> int:
+    need = C.c_uint64()
+    _check(lib().ap_gated_workspace(gate, up, n_tokens, need), "ap_gated_workspace")
+    return need.value
+
+
+def ap_gated(gate: ApWeights, up: ApWeights, x: ApVectors, h: ApVectors, n_tokens: int, act: int = AP_SILU, workspace_ptr: int = 0,
+             workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().ap_gated(gate, up, x, h, n_tokens, act, workspace_ptr, workspace_bytes, stream), "ap_gated")
+
+
+def ap_logprobs_workspace(logits: ApLogits, top: int = 0) -> int:
+    need = C.c_uint64()
+    _check(lib().ap_logprobs_workspace(logits, top, need), "ap_logprobs_workspace")
+    return need.value
+
+
+def ap_logprobs(logits: ApLogits, tokens_ptr: int, scale: float, top: int, logprob_ptr: int, entropy_ptr: int, top_id_ptr: int = 0,
+                top_logprob_ptr: int = 0, workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Device pointers; 0 for what is not asked for (``tokens`` with ``logprob``; ``entropy``)."""
+    _check(lib().ap_logprobs(logits, tokens_ptr, scale, top, logprob_ptr, entropy_ptr, top_id_ptr, top_logprob_ptr, workspace_ptr, workspace_bytes, stream),
+           "ap_logprobs")
