@@ -3,6 +3,7 @@
 
 #include "li_few.hpp"
 #include "li_logprobs.hpp"
+#include "li_many.hpp"
 #include "li_pack.hpp"
 
 namespace {
@@ -12,7 +13,7 @@ constexpr uint64_t kMostGroups = 1ull << 24;        // and workgroups (of 256 th
 
 bool multiple(const void* p, uint64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 bool stride_ok(int64_t s, int64_t n) { return s >= 0 && s % n == 0; }
-uint32_t tiles_of(uint64_t n, uint32_t tile) { return (uint32_t)((n + tile - 1) / tile); }
+uint32_t tiles_of(uint64_t n, uint64_t tile) { return (uint32_t)((n + tile - 1) / tile); }
 
 ap_status take_weights(const ap_weights* w, Weights* out) {
     if (!w || w->dtype > AP_FP16 || (w->group != 32 && w->group != 64 && w->group != 128)) return AP_ERR_INVALID;
@@ -61,33 +62,91 @@ ap_status pack_params(const ap_weights* weights, const ap_vectors* values, PackP
 }
 
 struct LinearPlan {
-    uint32_t token_tiles;
-    dim3 grid;
+    bool many;
+    uint32_t tokens;                                // of a workgroup
+    uint32_t part_blocks, n_parts;
+    uint32_t n_outs, n_tokens;                      // workgroups over the outputs and tokens
     uint64_t bytes;
 };
 
-constexpr uint32_t kFewOuts = 2;                    // tiles of outputs of a workgroup
+constexpr uint32_t kCus = 256;
 
-ap_status linear_plan(const Weights& w, uint32_t n_tokens, bool gated, LinearPlan* out) {
+// Up to kMostFew tokens go to the kernel of few rows, whose workgroup has all of them and 128 outputs or fewer; the other one's has
+// 512 outputs.  64 tokens, few / many, bf16, groups of 128, us: 4096 outputs of 4096 inputs 14.6 / 24.6, 4096 of 14336 26 / 37, 10240 of 8192
+// 32 / 42, gated 14336 of 4096 38 / 43.
+constexpr uint32_t kMostFew = 64;
+
+// Estimates of the kernel of many rows, us: what a workgroup's step of 128 columns takes besides its tiles of 16 tokens and for each
+// of them, what comes before the first and after the last step, what a second launch costs, and bytes of parts that are written and read a us.
+constexpr double kStepUs = 0.3, kTileUs = 0.46, kEnterUs = 8, kJoinUs = 4, kPartBytesPerUs = 4e6;
+
+ap_status linear_plan(const Weights& w, uint32_t n_tokens, uint32_t group, bool gated, LinearPlan* out) {
     LinearPlan r{};
     if (n_tokens >= kMost) return AP_ERR_RANGE;
-    r.token_tiles = n_tokens <= 16 ? 1 : n_tokens <= 32 ? 2 : 4;
-    const uint64_t outs = tiles_of(w.n_out, (gated ? kFewOuts / 2 : kFewOuts) * 16), tokens = tiles_of(n_tokens, r.token_tiles * 16);
-    if (outs >= kMostGroups / 2 || tokens >= 65536) return AP_ERR_RANGE;
-    r.grid = dim3((uint32_t)outs, (uint32_t)tokens);
+    const uint64_t tiles = (uint64_t)tiles_of(w.n_out, 16) * (gated ? 2 : 1), sums = (uint64_t)n_tokens * w.n_out * (gated ? 2 : 1);
+    r.many = n_tokens > kMostFew;
+    uint32_t parts = 1;
+    if (r.many) {
+        // Tiles of 64 or 96 tokens (64 for small groups, whose sums leave fewer registers), and the inputs in as many parts, as the estimate
+        // likes best: little in the tiles that is no token, workgroups that fill the chip in whole rounds, few parts to write and read.
+        r.n_outs = tiles_of(tiles, kManyTiles * kManyWaves);
+        double least = -1;
+        for (const uint32_t tokens : {96u, 64u}) {
+            if (tokens == 96 && group == 32) continue;
+            const double step_us = kStepUs + kTileUs * (tokens / 16);
+            for (uint32_t n = 1; n <= 32 && n <= w.blocks; ++n) {
+                const uint64_t rounds = ((uint64_t)r.n_outs * tiles_of(n_tokens, tokens) * n + kCus - 1) / kCus;
+                const double us = rounds * (tiles_of(w.blocks, n) * step_us + kEnterUs) + (n > 1 ? kJoinUs + 8.0 * n * sums / kPartBytesPerUs : 0.0);
+                if (least < 0 || us < least) least = us, parts = n, r.tokens = tokens;
+            }
+        }
+        r.n_tokens = tiles_of(n_tokens, r.tokens);
+    } else {
+        r.tokens = n_tokens <= 4 ? 4 : n_tokens <= 8 ? 8 : n_tokens <= 16 ? 16 : n_tokens <= 32 ? 32 : 64;
+        const uint32_t aside = r.tokens <= 16 ? (gated ? 2 : 1) : r.tokens / 8;
+        r.n_outs = tiles_of(tiles, aside), r.n_tokens = 1;
+        // With few outputs as many parts as fill the chip, of four steps each at least: 4096 outputs of 14336 inputs, 64 tokens, in 1, 3 and
+        // 8 parts 94, 41 and 26 us; 10240 of 8192 in 1, 2 and 3 56, 37 and 32 us.  Where a workgroup has few tokens it has its outputs in
+        // several tiles one after another, and no more workgroups are started than there are CUs.
+        parts = std::max<uint32_t>(1, std::min(kCus / std::min(kCus, r.n_outs), w.blocks * aside / 64));
+        if (r.tokens <= 16) r.n_outs = std::min(r.n_outs, kCus);
+    }
+    r.part_blocks = tiles_of(w.blocks, parts), r.n_parts = tiles_of(w.blocks, r.part_blocks);
+    if ((uint64_t)r.n_outs * r.n_tokens * r.n_parts >= kMostGroups / 4) return AP_ERR_RANGE;
+    if (r.n_parts > 1) r.bytes = 4ull * r.n_parts * sums;
     *out = r;
     return AP_OK;
 }
 
-ap_status run_linear(const LinearParams& p, const LinearPlan& plan, uint32_t dtype, uint32_t group, bool gated, hipStream_t on) {
+template <uint32_t... N, typename F> void for_one_of(uint32_t n, F f) { ((n == N ? f(std::integral_constant<uint32_t, N>{}) : void()), ...); }
+template <typename F> void for_truth(bool b, F f) { b ? f(std::true_type{}) : f(std::false_type{}); }
+
+ap_status run_linear(LinearParams p, const LinearPlan& plan, uint32_t dtype, uint32_t group, bool gated, void* workspace, hipStream_t on) {
+    p.parts = (float*)workspace, p.part_blocks = plan.part_blocks, p.n_parts = plan.n_parts;
     for_type(dtype, [&](auto e) {
         for_group(group, [&](auto g) {
-            using E = decltype(e);
-            auto pick = [&](auto tt) { return gated ? k_linear_few<E, g(), kFewOuts, tt(), true> : k_linear_few<E, g(), kFewOuts, tt(), false>; };
-            auto kernel = plan.token_tiles == 1 ? pick(std::integral_constant<uint32_t, 1>{}) : plan.token_tiles == 2 ? pick(std::integral_constant<uint32_t, 2>{})
-                                                                                                                   : pick(std::integral_constant<uint32_t, 4>{});
-            hipLaunchKernelGGL(kernel, plan.grid, dim3(kFewWaves * kLanes), 0, on, p);
+            for_truth(gated, [&](auto gates) {
+                for_truth(p.w[0].n_in % kBlock == 0, [&](auto whole) {
+                    using E = decltype(e);
+                    if (plan.many) {
+                        auto go = [&](auto tiles) {
+                            hipLaunchKernelGGL((k_linear_many<E, g(), tiles(), gates(), whole()>), dim3(plan.n_outs * plan.n_tokens * plan.n_parts), dim3(kManyWaves * kLanes), 0,
+                                               on, p, plan.n_outs, plan.n_tokens);
+                        };
+                        if (plan.tokens == 64) go(std::integral_constant<uint32_t, 4>{});
+                        else if constexpr (g() != 32) go(std::integral_constant<uint32_t, 6>{});
+                        return;
+                    }
+                    for_one_of<4, 8, 16, 32, 64>(plan.tokens, [&](auto t) {
+                        hipLaunchKernelGGL((k_linear_few<E, g(), t(), gates(), whole()>), dim3(plan.n_outs, 1, plan.n_parts), dim3(FewShape<g(), t(), gates()>::kWaves * kLanes), 0, on, p);
+                    });
+                });
+            });
         });
+        if (plan.n_parts > 1) {
+            auto join = gated ? k_join_parts<decltype(e), true> : k_join_parts<decltype(e), false>;
+            hipLaunchKernelGGL(join, dim3(tiles_of((uint64_t)p.n_tokens * p.w[0].n_out, 256)), dim3(256), 0, on, p);
+        }
     });
     return launched();
 }
@@ -151,7 +210,7 @@ ap_status ap_linear_workspace(const ap_weights* weights, uint32_t n_tokens, uint
     LinearPlan plan;
     if (!bytes) return AP_ERR_INVALID;
     ap_status st = take_weights(weights, &w);
-    if (st == AP_OK) st = linear_plan(w, n_tokens, false, &plan);
+    if (st == AP_OK) st = linear_plan(w, n_tokens, weights->group, false, &plan);
     if (st == AP_OK) *bytes = plan.bytes;
     return st;
 }
@@ -165,12 +224,12 @@ ap_status ap_linear(const ap_weights* weights, const ap_vectors* x, const ap_vec
     if (st == AP_OK) st = take_vectors(x, 16, &xs, &p.x_stride);
     if (st == AP_OK && add) st = take_vectors(add, 2, &adds, &p.add_stride);
     if (st == AP_OK) st = take_vectors(y, 2, &p.y, &p.y_stride);
-    if (st == AP_OK) st = linear_plan(p.w[0], n_tokens, false, &plan);
+    if (st == AP_OK) st = linear_plan(p.w[0], n_tokens, weights->group, false, &plan);
     if (st != AP_OK) return st;
     if (!space_ok(workspace, workspace_bytes, plan.bytes)) return AP_ERR_INVALID;
     if (n_tokens == 0) return AP_OK;
     p.x = xs, p.add = adds, p.n_tokens = n_tokens;
-    return run_linear(p, plan, weights->dtype, weights->group, false, (hipStream_t)stream);
+    return run_linear(p, plan, weights->dtype, weights->group, false, workspace, (hipStream_t)stream);
 }
 
 ap_status ap_gated_workspace(const ap_weights* gate, const ap_weights* up, uint32_t n_tokens, uint64_t* bytes) {
@@ -181,7 +240,7 @@ ap_status ap_gated_workspace(const ap_weights* gate, const ap_weights* up, uint3
     if (st == AP_OK) st = take_weights(up, &u);
     if (st != AP_OK) return st;
     if (gate->dtype != up->dtype || gate->group != up->group || g.n_out != u.n_out || g.n_in != u.n_in) return AP_ERR_INVALID;
-    st = linear_plan(g, n_tokens, true, &plan);
+    st = linear_plan(g, n_tokens, gate->group, true, &plan);
     if (st == AP_OK) *bytes = plan.bytes;
     return st;
 }
@@ -197,12 +256,12 @@ ap_status ap_gated(const ap_weights* gate, const ap_weights* up, const ap_vector
     if (st == AP_OK) st = take_vectors(h, 2, &p.y, &p.y_stride);
     if (st != AP_OK) return st;
     if (gate->dtype != up->dtype || gate->group != up->group || p.w[0].n_out != p.w[1].n_out || p.w[0].n_in != p.w[1].n_in || act > AP_GELU) return AP_ERR_INVALID;
-    st = linear_plan(p.w[0], n_tokens, true, &plan);
+    st = linear_plan(p.w[0], n_tokens, gate->group, true, &plan);
     if (st != AP_OK) return st;
     if (!space_ok(workspace, workspace_bytes, plan.bytes)) return AP_ERR_INVALID;
     if (n_tokens == 0) return AP_OK;
     p.x = xs, p.n_tokens = n_tokens, p.act = act;
-    return run_linear(p, plan, gate->dtype, gate->group, true, (hipStream_t)stream);
+    return run_linear(p, plan, gate->dtype, gate->group, true, workspace, (hipStream_t)stream);
 }
 
 ap_status ap_logprobs_workspace(const ap_logits* logits, uint32_t top, uint64_t* bytes) {

@@ -25,19 +25,54 @@ struct LinearParams {
     uint32_t part_blocks, n_parts;
 };
 
-// Eight codes of a word as 16 + code in the 16-bit type: a code's bits beside the exponent of 16 are that value exactly, so a
-// pair of them costs a shift and an and-or.
-template <typename E> __device__ __forceinline__ u32x4 codes16(uint32_t w) {
-    u32x4 r;
-    if constexpr (std::is_same_v<E, bf16>) {
-        r[0] = (w << 3 & 0x00780078u) | 0x41804180u, r[1] = (w >> 1 & 0x00780078u) | 0x41804180u;
-        r[2] = (w >> 5 & 0x00780078u) | 0x41804180u, r[3] = (w >> 9 & 0x00780078u) | 0x41804180u;
-    } else {
-        r[0] = (w << 6 & 0x03C003C0u) | 0x4C004C00u, r[1] = (w << 2 & 0x03C003C0u) | 0x4C004C00u;
-        r[2] = (w >> 2 & 0x03C003C0u) | 0x4C004C00u, r[3] = (w >> 6 & 0x03C003C0u) | 0x4C004C00u;
-    }
-    return r;
+// 16 bytes (4 bytes) of each lane from memory to LDS, from `from` + kOffset to the LDS address `to` + kOffset + 16 (4) * lane.  The data
+// passes no register, so that nothing here is in flight that the compiler could take for there; a wait for it has to come between it
+// and the barrier after which it is read.  (m0 says where in LDS: a reserved register, in which the compiler keeps nothing and which
+// it takes in no list of what a statement changes.)
+template <uint32_t kOffset> __device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off offset:%2" : : "s"(to), "v"(from), "n"(kOffset) : "memory");
 }
+__device__ __forceinline__ void load4_to_lds(const char* from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(to), "v"(from) : "memory");
+}
+// Until no more than n loads are on their way; until all reads of LDS have come.  (The compiler knows of the builtin.)
+template <uint32_t n> __device__ __forceinline__ void wait_loads() {
+    static_assert(n < 64);
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (n & 15) | (n >> 4) << 14);
+    asm volatile("" : : : "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    asm volatile("" : : : "memory");
+}
+
+// In LDS a row of an operand is 64 bytes, four pieces, which are turned by a number that goes by the row: the 16 lanes that a read takes
+// at once (lanes 0 to 3, 12 to 15 and 20 to 27; and so on) find theirs in 16 different places of 256 bytes.
+__device__ __forceinline__ uint32_t turned(uint32_t row, uint32_t piece) { return piece ^ (0x78u >> row / 4 * 2 & 3u); }
+// Likewise rows of 128 bytes, eight pieces.
+__device__ __forceinline__ uint32_t wide_turned(uint32_t row, uint32_t piece) { return piece ^ (row / 2 & 7u); }
+
+__device__ const u32x4 kZeros = {};                 // stands in for columns that are not there
+
+// Eight codes of a word as 16 + code in the 16-bit type: a code's bits beside the exponent of 16 are that value exactly, so a
+// pair of them costs a shift and an and-or.  That one takes no literals, and the compiler would split it in two: so the mask is
+// held in a scalar register and the exponents in a vector register.
+template <typename E> struct Unpack {
+    static constexpr bool kBf16 = std::is_same_v<E, bf16>;
+    uint32_t mask = kBf16 ? 0x00780078u : 0x03C003C0u, sixteen = kBf16 ? 0x41804180u : 0x4C004C00u;
+    __device__ __forceinline__ Unpack() {
+        asm volatile("" : "+s"(mask));
+        asm volatile("" : "+v"(sixteen));
+    }
+    __device__ __forceinline__ u32x4 operator()(uint32_t w) const {
+        u32x4 r;
+        if constexpr (kBf16) r[0] = w << 3, r[1] = w >> 1, r[2] = w >> 5, r[3] = w >> 9;
+        else r[0] = w << 6, r[1] = w << 2, r[2] = w >> 2, r[3] = w >> 6;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) r[i] = (r[i] & mask) | sixteen;
+        return r;
+    }
+};
 
 template <typename E> __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
     if constexpr (std::is_same_v<E, bf16>) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Vec8<bf16>, a), __builtin_bit_cast(Vec8<bf16>, b), c, 0, 0, 0);
@@ -60,6 +95,14 @@ template <typename E, bool kGated> __device__ __forceinline__ void finish(const 
     if constexpr (kGated) a = activated(a, p.act) * b;
     else if (p.add) a += load16<E>(p.add + (int64_t)t * p.add_stride + 2ull * n);
     store16<E>(p.y + (int64_t)t * p.y_stride + 2ull * n, a);
+}
+
+// The sums of a token and output: finished, or of a part as they are.
+template <typename E, bool kGated> __device__ __forceinline__ void put(const LinearParams& p, uint32_t part, uint32_t n, uint32_t t, float a, float b) {
+    if (p.n_parts == 1) return finish<E, kGated>(p, t, n, a, b);
+    float* row = p.parts + ((uint64_t)part * p.n_tokens + t) * ((kGated ? 2 : 1) * (uint64_t)p.w[0].n_out) + n;
+    row[0] = a;
+    if (kGated) row[p.w[0].n_out] = b;
 }
 
 }  // namespace

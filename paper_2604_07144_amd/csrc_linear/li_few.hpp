@@ -6,8 +6,13 @@
 // factors 16 + code are exact in the 16-bit type and so no weight is rounded; X is the product with a column of ones.  A
 // lane then has four tokens of one output, whose pair is the lane's own.
 //
-// A lane's 16 bytes of codes are what it multiplies in a block of 128 columns, so a wavefront reads 64 neighbouring bytes of 16 rows.
-// The wavefronts of a workgroup have the same outputs and take the blocks in turns, and their sums meet in LDS.
+// The lanes of an operand that lie next to each other are 16 different rows, and a load takes as many turns as it has such
+// places.  So codes, pairs and x come straight to LDS, lanes next to each other to a row's bytes next to each other, and from there to the
+// operands.  Several steps are on their way at once, in a ring.
+//
+// A workgroup's wavefronts are kAside that lie side by side over the outputs and share x (gated: half of them over gate, half over
+// up), times kDeep that take the blocks of 128 columns in turns; these meet in LDS at the end.  With few outputs the inputs are cut
+// into parts besides, whose sums k_join_parts adds up.
 #ifndef LI_FEW_HPP
 #define LI_FEW_HPP
 
@@ -15,98 +20,193 @@
 
 namespace {
 
-constexpr uint32_t kFewWaves = 8;
-
 template <typename E> constexpr uint32_t kOnes = std::is_same_v<E, bf16> ? 0x3F803F80u : 0x3C003C00u;
 
-// R tiles of 16 outputs (gated: half of them of gate, half of up), TT tiles of 16 tokens.
-template <typename E, uint32_t G, uint32_t R, uint32_t TT, bool kGated>
-__global__ __launch_bounds__(kFewWaves * kLanes) void k_linear_few(const LinearParams p) {
-    constexpr uint32_t kGroups = kBlock / G, kSteps = G / 32, kOuts = kGated ? R / 2 : R;
-    __shared__ f32x4 sums[kFewWaves][R * TT][kLanes];
+// Of a kernel for up to T tokens.
+template <uint32_t G, uint32_t T, bool kGated> struct FewShape {
+    static constexpr uint32_t kWaves = T == 8 || T == 16 ? 8 : 16, kTiles = T <= 16 ? 1 : T / 16, kAside = T <= 16 ? (kGated ? 2 : 1) : T / 8;
+    static constexpr uint32_t kDeep = kWaves / kAside, kOuts = kGated ? kAside / 2 : kAside;     // kOuts: tiles of 16 outputs side by side
+    static constexpr uint32_t kWords = kBlock / G, kPairLoads = (16 * kWords + kLanes - 1) / kLanes;
+    // x of a step and deep index: kTiles times 4 KiB, or of fewer than 16 tokens as many rows of 256 bytes; in loads of 1 KiB
+    static constexpr uint32_t kRows = T < 16 ? T : 16, kXBytes = kTiles * kRows * 256, kXLoads = (kXBytes / 1024 + kAside - 1) / kAside;
+    static constexpr uint32_t kLoads = 1 + kPairLoads + kXLoads;                                    // of a wavefront and step
+    static constexpr uint32_t kX = kDeep * kXBytes, kCodes = kWaves * 1024, kPairs = kWaves * kPairLoads * 256, kStage = kX + kCodes + kPairs;
+    static constexpr uint32_t kSumLanes = T < 16 ? T * 4 : kLanes;                                  // that have tokens
+    static constexpr bool kOneTile = T > 16;                                                        // a workgroup has one tile of outputs, not several
+    static constexpr uint32_t kSums = kWaves * kTiles * kSumLanes * 16, kApart = kOneTile ? 0 : kSums;   // in the ring, or beside it
+    static constexpr uint32_t kFit = (160 * 1024 - kApart) / kStage, kRing = kFit < 8 ? kFit : 8;
+    static constexpr uint32_t kLds = kApart + (kRing * kStage > kSums ? kRing * kStage : kSums);
+};
+
+// The wait for all but the `keep` newest steps of loads of `kLoads` each.
+template <uint32_t kLoads, uint32_t kMost> __device__ __forceinline__ void wait_steps(uint32_t keep) {
+    if constexpr (kMost > 0) {
+        if (keep < kMost) return wait_steps<kLoads, kMost - 1>(keep);
+    }
+    wait_loads<kLoads * kMost>();
+}
+
+template <typename E, uint32_t G, uint32_t T, bool kGated, bool kWhole>
+__global__ __launch_bounds__((FewShape<G, T, kGated>::kWaves * kLanes)) void k_linear_few(const LinearParams p) {
+    using Shape = FewShape<G, T, kGated>;
+    constexpr uint32_t TT = Shape::kTiles, kAside = Shape::kAside, kDeep = Shape::kDeep, kOuts = Shape::kOuts, kGroups = kBlock / G, kSteps = G / 32;
+    constexpr uint32_t kRing = Shape::kRing, kWords = Shape::kWords, kRows = Shape::kRows;
+    __shared__ __attribute__((aligned(16))) char lds[Shape::kLds];
     const uint32_t lane = threadIdx.x % kLanes, wave = uniform(threadIdx.x / kLanes), col = lane % 16, q = lane / 16;
-    const uint32_t n0 = blockIdx.x * (kOuts * 16), t0 = blockIdx.y * (TT * 16);
+    const uint32_t aside = wave % kAside, deep = wave / kAside;
+    const uint32_t begin = blockIdx.z * p.part_blocks, end = min(begin + p.part_blocks, p.w[0].blocks), steps = (end - begin + kDeep - 1) / kDeep;
+    const Weights& w = p.w[kGated ? aside / kOuts : 0];
 
-    const char *codes[R], *pairs[R];
-#pragma unroll
-    for (uint32_t r = 0; r < R; ++r) {
-        const Weights& w = p.w[kGated ? r / kOuts : 0];
-        const uint32_t n = min(n0 + (kGated ? r % kOuts : r) * 16 + col, w.n_out - 1);     // beyond the last: computed twice, not kept
-        codes[r] = w.codes + (int64_t)n * w.code_stride + q * 16;
-        pairs[r] = w.pairs + (int64_t)n * w.pair_stride;
-    }
-    const char* x[TT];
-    bool there[TT];
-#pragma unroll
-    for (uint32_t i = 0; i < TT; ++i) {
-        const uint32_t t = t0 + i * 16 + col;
-        there[i] = t < p.n_tokens;
-        x[i] = p.x + (int64_t)(there[i] ? t : 0u) * p.x_stride + q * 16;
-    }
+    // An even share of the outputs for each workgroup, and of those for each tile and wavefront: `rows` of them, which need not be the
+    // 16 that there is room for.
+    const uint32_t n_begin = (uint32_t)((uint64_t)w.n_out * blockIdx.x / gridDim.x), n_end = (uint32_t)((uint64_t)w.n_out * (blockIdx.x + 1) / gridDim.x);
+    const uint32_t tiles = Shape::kOneTile ? 1 : (n_end - n_begin + kOuts * 16 - 1) / (kOuts * 16);
+    const uint32_t rows = (n_end - n_begin + tiles * kOuts - 1) / (tiles * kOuts);
 
-    f32x4 acc[R][TT] = {};
-    for (uint32_t b = wave; b < p.w[0].blocks; b += kFewWaves) {
-        u32x4 c[R], a[TT][4];
-        PairWords<G> pr[R];
+    // A workgroup's steps begin at one of their own: rows are often some power of two apart, and all workgroups would come to the same
+    // memory channels at once.
+    const uint32_t first_step = blockIdx.x / 8 % steps;
+    uint32_t fill = 0, use = 0, load_step = first_step, load_left = steps, load_tile = 0;
+
+    // Codes: a lane has 16 bytes of row lane / 4.
+    const uint32_t slot = (col * 4 + turned(col, q)) * 16;
+    const char *codes, *pairs[Shape::kPairLoads];
+    auto enter = [&] {                                     // the rows of tile load_tile; beyond the wavefront's its last one again, not kept
+        const uint32_t n0 = n_begin + (load_tile * kOuts + aside % kOuts) * rows, n1 = min(min(n0 + rows, n_end), w.n_out) - 1;
+        codes = w.codes + (int64_t)min(n0 + lane / 4, n1) * w.code_stride + turned(lane / 4, lane % 4) * 16;
 #pragma unroll
-        for (uint32_t r = 0; r < R; ++r) {
-            c[r] = *reinterpret_cast<const u32x4*>(codes[r] + (int64_t)b * 64);
-            pr[r] = *reinterpret_cast<const PairWords<G>*>(pairs[r] + (int64_t)b * (4 * kGroups));
+        for (uint32_t i = 0; i < Shape::kPairLoads; ++i) {
+            const uint32_t e = min(i * kLanes + lane, 16 * kWords - 1);
+            pairs[i] = w.pairs + (int64_t)min(n0 + e / kWords, n1) * w.pair_stride + e % kWords * 4;
         }
+    };
+    enter();
+    // x: rows of 64 (fewer than 16 tokens) or 128 bytes, kRows of them for each 32 or 64 columns of a tile
+    constexpr uint32_t kRowLanes = T < 16 ? 4 : 8;
+    const char* x[Shape::kXLoads];
+    uint32_t x_col[Shape::kXLoads];                        // first column of a lane's piece in the block
+    uint32_t x_slot[2];                                    // where the lane's operand of 32 columns lies, in those, of even and odd ones
 #pragma unroll
-        for (uint32_t i = 0; i < TT; ++i)
+    for (uint32_t j = 0; j < Shape::kXLoads; ++j) {
+        const uint32_t e = (aside * Shape::kXLoads + j) * kLanes + lane;                    // piece of 16 bytes of all of the step's
+        const uint32_t in = e % (TT * kRows * 16), row = in / kRowLanes % kRows, part = in / kRowLanes / kRows;
+        if constexpr (T < 16) {
+            x_col[j] = part * 32 + turned(row, in % 4) * 8;
+            x[j] = p.x + (int64_t)min(row, p.n_tokens - 1) * p.x_stride + x_col[j] * 2;
+        } else {                                           // [tile][half of the columns][row]
+            const uint32_t at = part / 2 * 16 + row;
+            x_col[j] = part % 2 * 64 + wide_turned(row, in % 8) * 8;
+            x[j] = p.x + (int64_t)min(at, p.n_tokens - 1) * p.x_stride + x_col[j] * 2;
+        }
+    }
+    if constexpr (T < 16) x_slot[0] = x_slot[1] = (col % T * 4 + turned(col % T, q)) * 16;
+    else x_slot[0] = col * 128 + wide_turned(col, q) * 16, x_slot[1] = col * 128 + wide_turned(col, 4 + q) * 16;
+
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)lds;
+    const uint32_t base_x = base + deep * Shape::kXBytes + aside * Shape::kXLoads * 1024 % Shape::kXBytes, base_codes = base + Shape::kX + wave * 1024,
+                   base_pairs = base + Shape::kX + Shape::kCodes + wave * Shape::kPairLoads * 256;
+    auto load = [&] {
+        const uint32_t b = min(begin + load_step * kDeep + deep, end - 1);                  // behind the last block: the last one, not added
+        load_to_lds<0>(codes + (uint64_t)b * 64, base_codes + fill);
 #pragma unroll
-            for (uint32_t m = 0; m < 4; ++m) {
-                a[i][m] = u32x4{};
-                if (there[i] && b * kBlock + m * 32 + q * 8 < p.w[0].n_in) a[i][m] = *reinterpret_cast<const u32x4*>(x[i] + (int64_t)b * 256 + m * 64);
-            }
+        for (uint32_t i = 0; i < Shape::kPairLoads; ++i) load4_to_lds(pairs[i] + (uint64_t)b * (4 * kWords), base_pairs + fill + i * 256);
+#pragma unroll
+        for (uint32_t j = 0; j < Shape::kXLoads; ++j) {
+            const bool in = kWhole || b * kBlock + x_col[j] < p.w[0].n_in;
+            load_to_lds<0>(in ? x[j] + (uint64_t)b * 256 : (const char*)&kZeros, base_x + fill + j * 1024);
+        }
+        fill = fill == (kRing - 1) * Shape::kStage ? 0 : fill + Shape::kStage;
+        load_step = load_step + 1 == steps ? 0 : load_step + 1;
+        if (--load_left == 0) {
+            load_left = steps;
+            if (++load_tile < tiles) enter();
+        }
+    };
+    const Unpack<E> unpack;
+    f32x4 acc[TT] = {};
+    auto add = [&] {
+        const char* const at = lds + use;
+        const char* const at_x = at + deep * Shape::kXBytes;
+        const u32x4 c = *reinterpret_cast<const u32x4*>(at + Shape::kX + wave * 1024 + slot);
+        const PairWords<G> pr = *reinterpret_cast<const PairWords<G>*>(at + Shape::kX + Shape::kCodes + wave * Shape::kPairLoads * 256 + col * kWords * 4);
 #pragma unroll
         for (uint32_t g = 0; g < kGroups; ++g) {
-            f32x4 ones[TT];
+            f32x4 ones[TT] = {}, s[TT] = {};
+            const uint32_t one = kOnes<E>;
 #pragma unroll
-            for (uint32_t i = 0; i < TT; ++i) {
-                ones[i] = f32x4{};
+            for (uint32_t m = g * kSteps; m < (g + 1) * kSteps; ++m) {
+                u32x4 a[TT];
 #pragma unroll
-                for (uint32_t m = 0; m < kSteps; ++m) {
-                    const uint32_t one = kOnes<E>;
-                    ones[i] = mfma16<E>(a[i][g * kSteps + m], u32x4{one, one, one, one}, ones[i]);
-                }
+                for (uint32_t i = 0; i < TT; ++i) a[i] = *reinterpret_cast<const u32x4*>(at_x + (T < 16 ? m * (kRows * 64) : i * 4096 + m / 2 * 2048) + x_slot[m % 2]);
+#pragma unroll
+                for (uint32_t i = 0; i < TT; ++i) ones[i] = mfma16<E>(a[i], u32x4{one, one, one, one}, ones[i]);
+                const u32x4 v = unpack(c[m]);
+#pragma unroll
+                for (uint32_t i = 0; i < TT; ++i) s[i] = mfma16<E>(a[i], v, s[i]);
             }
+            const float step = low16<E>(pr[g]), low = fmaf(-16.0f, step, high16<E>(pr[g]));
 #pragma unroll
-            for (uint32_t r = 0; r < R; ++r) {
-                f32x4 s[TT] = {};
+            for (uint32_t i = 0; i < TT; ++i)
 #pragma unroll
-                for (uint32_t m = 0; m < kSteps; ++m) {
-                    const u32x4 w = codes16<E>(c[r][g * kSteps + m]);
+                for (uint32_t j = 0; j < 4; ++j) acc[i][j] = fmaf(step, s[i][j], fmaf(low, ones[i][j], acc[i][j]));
+        }
+    };
+    uint32_t use_step = first_step, use_left = steps, use_tile = 0;
+    auto leave = [&] {                                     // a tile is done: its sums meet, and each thread finishes single outputs
+        constexpr uint32_t kWide = Shape::kSumLanes, kTile = kWide * 4;
+        float* const sums = reinterpret_cast<float*>(lds + (Shape::kOneTile ? 0 : kRing * Shape::kStage));          // [wavefront][tile][lane][4]
+        __syncthreads();
+        if (lane < kWide)
 #pragma unroll
-                    for (uint32_t i = 0; i < TT; ++i) s[i] = mfma16<E>(a[i][g * kSteps + m], w, s[i]);
-                }
-                const float step = low16<E>(pr[r][g]), low = fmaf(-16.0f, step, high16<E>(pr[r][g]));
+            for (uint32_t i = 0; i < TT; ++i) *reinterpret_cast<f32x4*>(sums + (wave * TT + i) * kTile + lane * 4) = acc[i];
 #pragma unroll
-                for (uint32_t i = 0; i < TT; ++i)
+        for (uint32_t i = 0; i < TT; ++i) acc[i] = f32x4{};
+        __syncthreads();
+#pragma unroll 1
+        for (uint32_t e = threadIdx.x; e < kOuts * TT * kTile; e += Shape::kWaves * kLanes) {
+            const uint32_t u = e / kTile, w0 = u / TT, i = u % TT, l = e % kTile / 4;
+            const float* from = sums + (w0 * TT + i) * kTile + e % kTile;
+            float s = 0.0f, s2 = 0.0f;
 #pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j) acc[r][i][j] = fmaf(step, s[i][j], fmaf(low, ones[i][j], acc[r][i][j]));
+            for (uint32_t d = 0; d < kDeep; ++d) {
+                s += from[d * kAside * TT * kTile];
+                if (kGated) s2 += from[(d * kAside + kOuts) * TT * kTile];
             }
+            const uint32_t n0 = n_begin + (use_tile * kOuts + w0) * rows, n1 = min(min(n0 + rows, n0 + 16), n_end), n = n0 + l % 16, t = i * 16 + l / 16 * 4 + e % 4;
+            if (n < n1 && t < p.n_tokens) put<E, kGated>(p, blockIdx.z, n, t, s, s2);
         }
+        use_left = steps, ++use_tile;
+    };
+    auto arrived = [&] {
+        if constexpr (kAside > 1) __syncthreads();
+        else wait_lds();                                   // what is loaded next comes to where the last step was read
+    };
+    const uint32_t all = tiles * steps;
+    for (uint32_t i = 0; i < min(all, kRing - 1); ++i) load();
+    for (uint32_t i = 0; i < all; ++i) {
+        wait_steps<Shape::kLoads, kRing - 2>(min(all - 1 - i, kRing - 2));
+        arrived();
+        if (i + kRing - 1 < all) load();
+        if (begin + use_step * kDeep + deep < end) add();
+        use = use == (kRing - 1) * Shape::kStage ? 0 : use + Shape::kStage;
+        use_step = use_step + 1 == steps ? 0 : use_step + 1;
+        if (--use_left == 0) leave();
     }
-#pragma unroll
-    for (uint32_t r = 0; r < R; ++r)
-#pragma unroll
-        for (uint32_t i = 0; i < TT; ++i) sums[wave][r * TT + i][lane] = acc[r][i];
-    __syncthreads();
-    for (uint32_t u = wave; u < kOuts * TT; u += kFewWaves) {
-        f32x4 a{}, b{};
-#pragma unroll
-        for (uint32_t w = 0; w < kFewWaves; ++w) {
-            a += sums[w][u][lane];
-            if (kGated) b += sums[w][u + kOuts * TT][lane];
-        }
-        const uint32_t n = n0 + u / TT * 16 + col, t = t0 + u % TT * 16 + q * 4;
-        if (n < p.w[0].n_out)
-#pragma unroll
-            for (uint32_t j = 0; j < 4; ++j)
-                if (t + j < p.n_tokens) finish<E, kGated>(p, t + j, n, a[j], b[j]);
+}
+
+// Sums of the parts, in order.
+template <typename E, bool kGated> __global__ __launch_bounds__(256) void k_join_parts(const LinearParams p) {
+    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t t = (uint32_t)(at / p.w[0].n_out), n = (uint32_t)(at % p.w[0].n_out);
+    if (t >= p.n_tokens) return;
+    const uint64_t width = (kGated ? 2 : 1) * (uint64_t)p.w[0].n_out;
+    const float* from = p.parts + (uint64_t)t * width + n;
+    float a = 0.0f, b = 0.0f;
+    for (uint32_t z = 0; z < p.n_parts; ++z, from += (uint64_t)p.n_tokens * width) {
+        a += from[0];
+        if (kGated) b += from[p.w[0].n_out];
     }
+    finish<E, kGated>(p, t, n, a, b);
 }
 
 }  // namespace
