@@ -153,6 +153,7 @@ ap_status run_linear(LinearParams p, const LinearPlan& plan, uint32_t dtype, uin
 
 bool space_ok(const void* workspace, uint64_t bytes, uint64_t need) { return need == 0 || (workspace && multiple(workspace, 16) && bytes >= need); }
 
+constexpr uint32_t kMostPieces = 16;                // one for each wavefront that joins them
 struct LogPlan {
     uint32_t pieces, piece;
     uint64_t bytes;
@@ -164,9 +165,9 @@ ap_status take_logits(const ap_logits* x, uint32_t top, LogPlan* out) {
     if (!multiple(x->data, size) || !stride_ok(x->stride, size)) return AP_ERR_INVALID;
     if (x->vocab >= kMost || x->n_rows >= kMost) return AP_ERR_RANGE;
     LogPlan r{};
-    r.pieces = 1;
-    while (r.pieces < 32 && (uint64_t)x->n_rows * r.pieces < 512 && x->vocab / r.pieces > 8192) r.pieces *= 2;
-    r.piece = (tiles_of(x->vocab, r.pieces) + 7) / 8 * 8;
+    // Few rows are cut into pieces of whole spans of a workgroup, so that 1024 workgroups have something to do.
+    const uint32_t units = tiles_of(x->vocab, kLogWaves * kSpan), groups = 1024 / std::min<uint32_t>(1024, std::max<uint32_t>(1, x->n_rows));
+    r.piece = tiles_of(units, std::max<uint32_t>(1, std::min(std::min(groups, units), kMostPieces))) * kLogWaves * kSpan;
     r.pieces = tiles_of(x->vocab, r.piece);
     if ((uint64_t)x->n_rows * r.pieces >= kMostGroups) return AP_ERR_RANGE;
     if (r.pieces > 1) r.bytes = (uint64_t)x->n_rows * r.pieces * (16 + 8ull * top);
@@ -277,19 +278,19 @@ ap_status ap_logprobs(const ap_logits* logits, const int32_t* tokens, float scal
     LogPlan plan;
     const ap_status st = take_logits(logits, top, &plan);
     if (st != AP_OK) return st;
-    if (!(scale > 0.0f) || !std::isfinite(scale * kLog2e) || (tokens == nullptr) != (logprob == nullptr) || (top && (!top_id || !top_logprob))) return AP_ERR_INVALID;
+    if (!(scale * kLog2e > 0.0f) || !std::isfinite(scale * kLog2e) || (tokens == nullptr) != (logprob == nullptr) || (top && (!top_id || !top_logprob))) return AP_ERR_INVALID;
     if (!multiple(tokens, 4) || !multiple(logprob, 4) || !multiple(entropy, 4) || (top && (!multiple(top_id, 4) || !multiple(top_logprob, 4)))) return AP_ERR_INVALID;
     if (!space_ok(workspace, workspace_bytes, plan.bytes)) return AP_ERR_INVALID;
     if (logits->n_rows == 0) return AP_OK;
     LogParams p{};
     p.logits = (const char*)logits->data, p.stride = logits->stride, p.n_rows = logits->n_rows, p.vocab = logits->vocab;
     p.top = top, p.pieces = plan.pieces, p.piece = plan.piece;
-    p.tokens = tokens, p.scale = scale, p.logprob = logprob, p.entropy = entropy, p.top_logprob = top_logprob, p.top_id = top_id;
-    p.part_sums = (f32x4*)workspace, p.part_keys = (uint64_t*)((char*)workspace + (uint64_t)p.n_rows * p.pieces * 16);
+    p.tokens = tokens, p.c = scale * kLog2e, p.logprob = logprob, p.entropy = entropy, p.top_logprob = top_logprob, p.top_id = top_id;
+    p.part_sums = (Sums*)workspace, p.part_keys = (uint64_t*)((char*)workspace + (uint64_t)p.n_rows * p.pieces * 16);
     for_logits(logits->dtype, [&](auto e) {
         using E = decltype(e);
         hipLaunchKernelGGL((k_logprobs<E>), dim3(p.n_rows * p.pieces), dim3(kLogThreads), 0, (hipStream_t)stream, p);
-        if (p.pieces > 1) hipLaunchKernelGGL((k_join_logprobs<E>), dim3(p.n_rows), dim3(kLogThreads), 0, (hipStream_t)stream, p);
+        if (p.pieces > 1) hipLaunchKernelGGL((k_join_logprobs<E>), dim3(p.n_rows), dim3(kJoinWaves * kLanes), 0, (hipStream_t)stream, p);
     });
     return launched();
 }

@@ -79,6 +79,23 @@ template <typename E> __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, 
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(Vec8<fp16>, a), __builtin_bit_cast(Vec8<fp16>, b), c, 0, 0, 0);
 }
 
+// The number of lane ^ M.
+template <uint32_t M> __device__ __forceinline__ uint32_t across(uint32_t x) {
+    if constexpr (M == 1) return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true);              // quads 1 0 3 2
+    else if constexpr (M == 2) return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true);         // quads 2 3 0 1
+    else if constexpr (M == 4) return (uint32_t)__builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xF, 0xF, true), 0x1B, 0xF, 0xF, true);   // 8 turned round, quads turned round
+    else if constexpr (M == 8) return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xF, 0xF, true);        // 16 moved on by 8
+    else if constexpr (M == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    }
+}
+template <uint32_t M> __device__ __forceinline__ float across(float x) { return __uint_as_float(across<M>(__float_as_uint(x))); }
+template <uint32_t M> __device__ __forceinline__ uint64_t across(uint64_t x) { return (uint64_t)across<M>((uint32_t)(x >> 32)) << 32 | across<M>((uint32_t)x); }
+
 // The bytes of a block's pairs, as words (one for each group).
 template <uint32_t G> using PairWords = uint32_t __attribute__((ext_vector_type(kBlock / G)));
 

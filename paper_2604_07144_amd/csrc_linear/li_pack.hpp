@@ -47,29 +47,47 @@ template <typename E, uint32_t G> __global__ __launch_bounds__(kPackThreads) voi
     }
 #pragma unroll
     for (uint32_t u = 0; u < kPackUnits; ++u) {
-        float lo = INFINITY, hi = -INFINITY;
-        uint32_t odd = 0;
+        float lo = INFINITY, hi = -INFINITY, numbers = 0.0f;
         if (at[u].inside) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float a = low16<E>(x[u][i]), b = high16<E>(x[u][i]);
-                lo = fminf(lo, fminf(a, b)), hi = fmaxf(hi, fmaxf(a, b));
-                odd |= !(fabsf(a) < INFINITY) || !(fabsf(b) < INFINITY);
+                lo = fminf(fminf(lo, a), b), hi = fmaxf(fmaxf(hi, a), b);
+                numbers = fmaf(a, 0.0f, fmaf(b, 0.0f, numbers));       // NaN as soon as one is not a number
             }
         }
-        uint32_t some = at[u].inside;
-#pragma unroll
-        for (uint32_t m = 1; m < G / 8; m *= 2) {
-            lo = fminf(lo, __shfl_xor(lo, m)), hi = fmaxf(hi, __shfl_xor(hi, m));
-            odd |= __shfl_xor(odd, m), some |= __shfl_xor(some, m);
-        }
-        const uint32_t pair = some ? group_pair<E>(lo, hi, !odd) : 0u;
+        uint32_t odd = numbers != numbers;
+        odd |= at[u].inside ? 2u : 0u;                      // bit 0: not all are numbers; bit 1: there are some
+        auto widen = [&](auto m) {
+            lo = fminf(lo, across<m()>(lo)), hi = fmaxf(hi, across<m()>(hi));
+            odd |= across<m()>(odd);
+        };
+        widen(std::integral_constant<uint32_t, 1>{}), widen(std::integral_constant<uint32_t, 2>{});
+        if constexpr (G >= 64) widen(std::integral_constant<uint32_t, 4>{});
+        if constexpr (G >= 128) widen(std::integral_constant<uint32_t, 8>{});
+        const uint32_t pair = odd & 2 ? group_pair<E>(lo, hi, !(odd & 1)) : 0u;
         const float step = low16<E>(pair), low = high16<E>(pair);
+        // As code_of, without a division for each value: with the inverse of the step rounded to the nearest, one step of correction makes
+        // a product the quotient rounded to the nearest.  Steps near the ends of the range are left to code_of.
         uint32_t word = 0;
         if (at[u].inside) {
+            const float d = step * 0.0625f, from = low * -0.0625f, near = __builtin_amdgcn_rcpf(d), inverse = fmaf(fmaf(-d, near, 1.0f), near, near);
+            if (d > 0x1p-90f && d < 0x1p90f) {
+                float even = 0.0f, odds = 0.0f;                        // codes as digits: whole numbers below 2^16
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                word |= code_of(low16<E>(x[u][i]), low, step) << (4 * i) | code_of(high16<E>(x[u][i]), low, step) << (4 * i + 16);
+                for (int i = 0; i < 4; ++i) {
+                    auto code = [&](float v) {
+                        const float n = fmaf(v, 0.0625f, from), q = n * inverse;
+                        return fminf(fmaxf(rintf(fmaf(fmaf(-d, q, n), inverse, q)), 0.0f), 15.0f);
+                    };
+                    even = fmaf(code(low16<E>(x[u][i])), (float)(1 << 4 * i), even), odds = fmaf(code(high16<E>(x[u][i])), (float)(1 << 4 * i), odds);
+                }
+                word = (uint32_t)even | (uint32_t)odds << 16;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    word |= code_of(low16<E>(x[u][i]), low, step) << (4 * i) | code_of(high16<E>(x[u][i]), low, step) << (4 * i + 16);
+            }
         }
         if (at[u].there) {
             reinterpret_cast<uint32_t*>(p.w.codes + (int64_t)at[u].row * p.w.code_stride + (int64_t)at[u].block * (kBlock / 2))[word_of(at[u].lane)] = word;

@@ -115,3 +115,18 @@ def test_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(words, want) and (back - x).abs().max() < 0.5
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("scale", [1e-30, 1e-4, 1.0, 1e4, 1e30])
+def test_values_of_any_size(dtype, scale):
+    """Steps from next to nothing to next to overflow, and values that lie in the middle between two codes."""
+    if dtype == "fp16" and not 1e-4 <= scale <= 1e3:
+        pytest.skip("beyond the type's range")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(7)
+    x = (scale * torch.randn((64, 512), generator=gen, device="cuda")).to(TYPES[dtype][0])
+    x[32:] = (scale * (torch.randint(0, 31, (32, 512), generator=gen, device="cuda") / 2.0)).to(x.dtype)
+    words, pairs, w, _keep = _pack(x, 64, dtype)
+    codes, want = orc.packed(x.double().cpu().numpy(), 64, _up(x.dtype))
+    assert np.array_equal(pairs.double().cpu().numpy(), want) and np.array_equal(_codes(words, 512)[0], codes)
