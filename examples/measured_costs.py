@@ -1,10 +1,10 @@
 """Score candidate assignments with costs measured on this card.
 
-    python examples/measured_costs.py [--bits 4] [--candidates 64] [--window 4096 --sinks 4]
+    python examples/measured_costs.py [--bits 4] [--weights4] [--candidates 64] [--window 4096 --sinks 4]
 
 Runs one layer of a served model (paged cache, position rotation, attention) on the GPU at a grid of lengths, puts the measured
 times in the place of the roofline's attention term, and scores the same candidates with the roofline's cost tables and with the
-measured ones.  The model is an 8B-class one (32 layers, 32 heads on 8), the trace the small synthetic one; the weights and rows
+measured ones.  With --weights4 the projections, the feed-forward block and the output head are held in 4 bits and measured too.  The model is an 8B-class one (32 layers, 32 heads on 8), the trace the small synthetic one; the weights and rows
 are random, which no time here depends on.
 """
 import argparse
@@ -40,6 +40,7 @@ def main(argv=None):
     p.add_argument("--bits", type=int, choices=(16, 4), default=16, help="what the cache is held in")
     p.add_argument("--window", type=int, default=0, help="sliding window of the attention (0: none)")
     p.add_argument("--sinks", type=int, default=0, help="first tokens that stay visible beside the window")
+    p.add_argument("--weights4", action="store_true", help="weights in 4 bits, measured too")
     p.add_argument("--candidates", type=int, default=64)
     a = p.parse_args(argv)
     tr = traces.make_trace(0)
@@ -52,7 +53,10 @@ def main(argv=None):
     w = binding.ap_workload_create(tr.arrival_us, tr.prompt_len, tr.out_len)
     roofline = binding.ap_roofline_costs(w, len(tr.prompt_len), np.array([MODEL]), np.array([GPU]), np.array([(0, 0, 1, tr.B)], binding.GROUP_DTYPE))
     binding.ap_workload_destroy(w)
-    tables = measured.request_tables(MODEL, GPU, tr.B, tr.prompt_len, tr.out_len, grid, decode_us, grid, prefill_us)
+    weights = measured.weight_times(MODEL, tr.B, grid) if a.weights4 else None
+    if weights:
+        print(f"one layer's weights in 4 bits: decode step {weights[0]:.1f} us, prefill of {grid[-1]} tokens {weights[1][-1]:.1f}; output head {weights[2]:.1f}")
+    tables = measured.request_tables(MODEL, GPU, tr.B, tr.prompt_len, tr.out_len, grid, decode_us, grid, prefill_us, weights)
     for name, t in (("roofline", roofline), ("measured", tables)):
         m = score(tr, t[:2], a.candidates)
         print(f"{name}: mean TTFT {m['sum_ttft_us'].mean() / len(tr.prompt_len) / 1e3:8.2f} ms, mean TPOT {m['sum_tpot_us'].mean() / len(tr.prompt_len) / 1e3:7.3f} ms, "

@@ -1,9 +1,11 @@
-"""Cost tables with the cache and attention measured on the card.
+"""Cost tables with a replica's step measured on the card.
 
 The roofline prices every operator of a model analytically.  What goes by the lengths in a trace is the cache of keys and
 values and the attention over it; this module runs those (``ap_kv_append``, ``ap_attention``) on the present device at a grid of
 lengths and puts the measured times in the place of the roofline's attention term, so that ``ap_costtable_set`` can score
-candidates with them.  Projections, output head and all-reduce stay the roofline's.
+candidates with them.  For replicas whose weights are held in 4 bits the projections and feed-forward blocks (``ap_linear``,
+``ap_gated``) and the output head with its answer (``ap_linear``, ``ap_logprobs``) can be measured alike; what is not stays the
+roofline's, as the all-reduce does.
 """
 from __future__ import annotations
 
@@ -87,22 +89,126 @@ class ReplicaLayer:
         other memory."""
         with torch.cuda.device(self.device):
             p = self.plan(held, new)
-            self.step(p)
-            graph = torch.cuda.CUDAGraph()
-            with torch.cuda.graph(graph):
-                for _ in range(repeats):
-                    self.step(p)
-            other, times = torch.zeros(2 * CHIP_CACHE // 4, dtype=torch.int32, device=self.device), []
-            graph.replay()
-            for _ in range(5):
-                a, z = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-                other.sum()                                     # also keeps the device busy until what is timed has been sent
-                a.record()
-                graph.replay()
-                z.record()
-                z.synchronize()
-                times.append(a.elapsed_time(z) * 1e3 / repeats)
-        return float(np.median(times))
+            return _graph_us(lambda: self.step(p), repeats, self.device)
+
+
+def _graph_us(step, repeats: int, device) -> float:
+    """Median of five timings of ``repeats`` steps in a graph, microseconds a step; other memory fills the chip's caches before each."""
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(repeats):
+            step()
+    other, times = torch.zeros(2 * CHIP_CACHE // 4, dtype=torch.int32, device=device), []
+    graph.replay()
+    for _ in range(5):
+        a, z = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        other.sum()                                     # also keeps the device busy until what is timed has been sent
+        a.record()
+        graph.replay()
+        z.record()
+        z.synchronize()
+        times.append(a.elapsed_time(z) * 1e3 / repeats)
+    return float(np.median(times))
+
+
+class ReplicaWeights:
+    """Matrices of a model in 4 bits, ``copies`` times, and steps of ``n_tokens`` rows through them: a layer's projections and
+    feed-forward block (``layer``), or the output head with the log probabilities of its ``top`` alternatives (``head``).
+
+    ``model`` is a record of ``binding.MODEL_DTYPE``; ``group`` columns share a pair.  The values are random, which no time depends on.
+    Steps take turns at the copies, so that each comes back to its weights only after all the others."""
+
+    def __init__(self, model, *, head: bool = False, top: int = 0, dtype: str = "bf16", group: int = 128, copies: int = 1, device: str = "cuda", seed: int = 0):
+        H, A, K = (int(model[f]) for f in ("hidden", "heads", "kv_heads"))
+        d = H // A
+        self.torch_dtype, self.dtype = DTYPES[dtype]
+        self.hidden, self.group, self.head, self.top = H, group, head, top
+        self.device = device = torch.empty(0, device=device).device    # with its number
+        self.gen = torch.Generator(device=device)
+        self.gen.manual_seed(seed)
+        sizes = dict(head=(int(model["vocab"]), H)) if head else \
+            dict(qkv=((A + 2 * K) * d, H), out=(H, A * d), gate=(int(model["intermediate"]), H), up=(int(model["intermediate"]), H), down=(H, int(model["intermediate"])))
+        with torch.cuda.device(device):
+            self.copies = [{f: self._packed(*size) for f, size in sizes.items()} for _ in range(copies)]
+        self.sizes = sizes
+
+    def _packed(self, n_out: int, n_in: int) -> dict:
+        values = (n_in ** -0.5 * torch.randn((n_out, n_in), generator=self.gen, device=self.device)).to(self.torch_dtype)
+        codes, pairs = binding.weight_row_bytes(self.group, n_in)
+        w = dict(codes=torch.empty((n_out, codes), dtype=torch.uint8, device=self.device), pairs=torch.empty((n_out, pairs), dtype=torch.uint8, device=self.device))
+        w["w"] = binding.make_weights(self.dtype, self.group, n_out, n_in, w["codes"].data_ptr(), w["pairs"].data_ptr())
+        binding.ap_weights_pack(w["w"], binding.make_vectors(values.data_ptr(), n_in), torch.cuda.current_stream().cuda_stream)
+        return w
+
+    def bytes(self) -> int:
+        """Of one copy."""
+        return sum(x.numel() for w in self.copies[0].values() for x in (w["codes"], w["pairs"]))
+
+    def plan(self, n_tokens: int) -> dict:
+        """Rows, descriptions and workspace of steps of ``n_tokens`` rows: ``x`` goes in, ``y`` comes out (``logits`` and the answers)."""
+        if n_tokens < 1:
+            raise ValueError(f"a step of {n_tokens} tokens")
+        rows = lambda n: torch.zeros((n_tokens, n), dtype=self.torch_dtype, device=self.device)    # noqa: E731
+        p = dict(n=n_tokens, at=0, x=torch.randn((n_tokens, self.hidden), generator=self.gen, device=self.device).to(self.torch_dtype))
+        w = {f: c["w"] for f, c in self.copies[0].items()}
+        with torch.cuda.device(self.device):
+            if self.head:
+                vocab = self.sizes["head"][0]
+                wide = -(-vocab // 8) * 8                  # rows of logits begin at multiples of 16 bytes
+                p["y"] = rows(wide)
+                p["logits"] = binding.make_logits(self.dtype, n_tokens, vocab, p["y"].data_ptr(), 2 * wide)
+                p["tokens"] = torch.zeros(n_tokens, dtype=torch.int32, device=self.device)
+                p["logprob"], p["entropy"] = (torch.zeros(n_tokens, device=self.device) for _ in range(2))
+                p["top_id"], p["top_logprob"] = (torch.zeros((n_tokens, self.top), dtype=t, device=self.device) for t in (torch.int32, torch.float32))
+                need = [binding.ap_linear_workspace(w["head"], n_tokens), binding.ap_logprobs_workspace(p["logits"], self.top)]
+            else:
+                for f in ("qkv", "gate"):
+                    p[f] = rows(self.sizes[f][0])
+                p["attended"] = torch.randn((n_tokens, self.sizes["out"][1]), generator=self.gen, device=self.device).to(self.torch_dtype)
+                p["mid"], p["y"] = rows(self.hidden), rows(self.hidden)
+                need = [binding.ap_linear_workspace(w[f], n_tokens) for f in ("qkv", "out", "down")] + [binding.ap_gated_workspace(w["gate"], w["up"], n_tokens)]
+            p["space"] = torch.empty(max(16, *need), dtype=torch.uint8, device=self.device)
+        p["rows"] = {f: binding.make_vectors(p[f].data_ptr(), p[f].shape[1]) for f in ("x", "y", "qkv", "gate", "attended", "mid") if f in p}
+        return p
+
+    def step(self, p: dict) -> torch.Tensor:
+        """A layer: queries, keys and values of ``x`` (to ``qkv``); ``attended`` projected onto ``x``; the feed-forward block onto that.  The
+        head: logits of ``x``, and what they say of ``tokens``."""
+        w, rows, n, b = {f: c["w"] for f, c in self.copies[p["at"]].items()}, p["rows"], p["n"], binding
+        p["at"] = (p["at"] + 1) % len(self.copies)
+        with torch.cuda.device(self.device):
+            tail = (p["space"].data_ptr(), p["space"].numel(), torch.cuda.current_stream().cuda_stream)
+            if self.head:
+                b.ap_linear(w["head"], rows["x"], rows["y"], n, None, *tail)
+                b.ap_logprobs(p["logits"], p["tokens"].data_ptr(), 1.0, self.top, p["logprob"].data_ptr(), p["entropy"].data_ptr(),
+                              p["top_id"].data_ptr(), p["top_logprob"].data_ptr(), *tail)
+            else:
+                b.ap_linear(w["qkv"], rows["x"], rows["qkv"], n, None, *tail)
+                b.ap_linear(w["out"], rows["attended"], rows["mid"], n, rows["x"], *tail)
+                b.ap_gated(w["gate"], w["up"], rows["mid"], rows["gate"], n, b.AP_SILU, *tail)
+                b.ap_linear(w["down"], rows["gate"], rows["y"], n, rows["mid"], *tail)
+        return p["y"]
+
+    def time_us(self, n_tokens: int, repeats: int = 20) -> float:
+        """Microseconds of a step among others, as ``ReplicaLayer.time_us``."""
+        with torch.cuda.device(self.device):
+            p = self.plan(n_tokens)
+            return _graph_us(lambda: self.step(p), repeats, self.device)
+
+
+def weight_times(model, batch: int, prompts, *, dtype: str = "bf16", group: int = 128, top: int = 0, repeats: int = 20):
+    """Measured microseconds of a layer's projections and feed-forward block with weights in 4 bits: of a decode step of ``batch``
+    sequences, of prefills of ``batch`` prompts of each of ``prompts`` (an array); and of the output head on ``batch`` rows with the log
+    probabilities of ``top`` alternatives."""
+    def of(head):
+        one = ReplicaWeights(model, head=head, top=top, dtype=dtype, group=group)
+        copies = max(1, min(repeats, -(-2 * CHIP_CACHE // one.bytes())))         # the chip's caches do not hold them
+        return one if copies == 1 else ReplicaWeights(model, head=head, top=top, dtype=dtype, group=group, copies=copies)
+
+    layer = of(False)
+    decode, prefill = layer.time_us(batch, repeats), np.array([layer.time_us(batch * int(s), max(2, repeats // 4)) for s in prompts])
+    return decode, prefill, of(True).time_us(batch, repeats)
 
 
 def layer_times(model, batch: int, contexts, prompts, *, dtype: str = "bf16", bits: int = 16, page: int = 16, window: int = 0,
@@ -123,6 +229,26 @@ def _roofline_attention_us(model, gpu, batch, n, c):
     A, K, d, e = float(model["heads"]), float(model["kv_heads"]), float(model["hidden"]) / float(model["heads"]), float(model["weight_bits"]) / 8.0
     flops, nbytes = 4.0 * batch * n * c * A * d, e * (2.0 * batch * n * A * d + 2.0 * batch * c * K * d)
     return flops / np.minimum(flops / nbytes * gpu["hbm_bytes_per_s"], gpu["flops"]) * 1e6
+
+
+def _op_us(gpu, flops, nbytes):
+    return flops / np.minimum(flops / nbytes * gpu["hbm_bytes_per_s"], gpu["flops"]) * 1e6
+
+
+def _roofline_weights_us(model, gpu, batch, n):
+    """The roofline's time of one layer's projections and feed-forward block: n new tokens a sequence."""
+    H, I, A, K, e, b = *(float(model[f]) for f in ("hidden", "intermediate", "heads", "kv_heads")), float(model["weight_bits"]) / 8.0, float(batch)
+    d = H / A
+    wide = (A + 2.0 * K) * d
+    return _op_us(gpu, 2.0 * b * n * H * wide, e * (H * wide + b * n * H + b * n * wide)) + \
+        _op_us(gpu, 2.0 * b * n * A * d * H, e * (A * d * H + b * n * A * d + b * n * H)) + \
+        _op_us(gpu, 6.0 * b * n * H * I, e * (3.0 * H * I + 2.0 * b * n * H + 3.0 * b * n * I))
+
+
+def _roofline_head_us(model, gpu, batch):
+    """The roofline's time of the output head on the last position of each sequence."""
+    H, V, e, b = float(model["hidden"]), float(model["vocab"]), float(model["weight_bits"]) / 8.0, float(batch)
+    return _op_us(gpu, 2.0 * b * H * V, e * (H * V + b * H + b * V))
 
 
 def _times(grid, us, longest, what):
@@ -153,9 +279,11 @@ def _between(length, grid, us):
     return np.clip(y, np.minimum(us[i], us[i + 1]), np.maximum(us[i], us[i + 1]))
 
 
-def request_tables(model, gpu, batch: int, prompt_len, out_len, contexts, decode_us, prompts, prefill_us):
+def request_tables(model, gpu, batch: int, prompt_len, out_len, contexts, decode_us, prompts, prefill_us, weights=None):
     """``prefill_us`` and ``tpot_us`` (uint32 [1][R], for ``ap_costtable_set``) of requests on a replica of one GPU: the roofline's
     times with its attention term replaced by the measured ones, interpolated by parabolas between the lengths they were taken at.
+    With ``weights``, what ``weight_times`` gives for the same ``prompts``, the terms of projections, feed-forward block and head are
+    replaced too.
 
     Lengths ascend and reach the longest prompt (``prompts``) and the longest context of a decode step (``contexts``), otherwise
     ValueError; what is shorter than the first length takes the first time."""
@@ -170,6 +298,14 @@ def request_tables(model, gpu, batch: int, prompt_len, out_len, contexts, decode
     change = lambda grid, us, n: layers * (_between(length, grid, us) - _roofline_attention_us(model, gpu, batch, n, length))   # noqa: E731
     pre = np.asarray(pre_ns, np.float64).reshape(-1)[1:longest + 1] / 1e3 + change(prompts, prefill_us, length)
     step = np.diff(np.asarray(prefix_ns, np.float64).reshape(-1))[1:longest + 1] / 1e3 + change(contexts, decode_us, 1.0)
+    if weights is not None:
+        w_decode, w_prefill, w_head = weights
+        _, w_prefill = _times(prompts, w_prefill, int(prompt.max()), "prefills' weights")
+        if not (np.isfinite([w_decode, w_head]).all() and min(w_decode, w_head) >= 0):
+            raise ValueError("weights: times have to be numbers that are not negative")
+        head = float(w_head) - _roofline_head_us(model, gpu, batch)
+        pre = pre + layers * (_between(length, prompts, w_prefill) - _roofline_weights_us(model, gpu, batch, length)) + head
+        step = step + layers * (float(w_decode) - _roofline_weights_us(model, gpu, batch, 1.0)) + head
     upto = np.concatenate([[0.0], np.cumsum(step)])          # of contexts 1 .. k
     tpot = (upto[prompt + out - 1] - upto[prompt - 1]) / out
     whole = lambda x: np.maximum(1, np.rint(x)).astype(np.uint32)[None]   # noqa: E731
