@@ -1,23 +1,10 @@
 // C ABI of the cache and attention operators: checks of arguments, choice of kernels and grids.
 #include "at_append.hpp"
 #include "at_few.hpp"
+#include "at_host.hpp"
 #include "at_many.hpp"
 
 namespace {
-
-constexpr uint64_t kMost = 1ull << 31;   // rows and positions stay below
-constexpr uint64_t kMostGroups = 1ull << 24;  // and workgroups (of 256 threads: a grid holds less than 2^32)
-
-bool multiple(const void* p, uint64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-bool stride_ok(int64_t s, int64_t n) { return s >= 0 && s % n == 0; }
-
-// magic and shift of a division of numbers below 2^31 by `d`: n / d = ((2 n) * magic >> 32) >> shift
-void divider(uint32_t d, uint32_t* magic, uint32_t* shift) {
-    uint32_t l = 0;
-    while ((1ull << l) < d) ++l;
-    *shift = l;
-    *magic = (uint32_t)(((1ull << (31 + l)) + d - 1) / d);
-}
 
 ap_status take_cache(const ap_kv_cache* c, Cache* out) {
     if (!c || c->dtype > AP_FP16 || (c->bits != 16 && c->bits != 4) || (c->head_dim != 64 && c->head_dim != 128)) return AP_ERR_INVALID;
@@ -58,8 +45,6 @@ template <typename F> void for_bits(uint32_t b, F f) { b == 16 ? f(std::integral
 template <typename F> void for_cache(const ap_kv_cache* c, F f) {
     for_type(c->dtype, [&](auto e) { for_dim(c->head_dim, [&](auto d) { for_bits(c->bits, [&](auto b) { f(e, d, b); }); }); });
 }
-
-ap_status launched() { return hipGetLastError() == hipSuccess ? AP_OK : AP_ERR_DEVICE; }
 
 // Heads that a wavefront takes one after another: with few tokens a pass each, so that the call is as short as one pass;
 // with many up to four, which share the look-up of the token and its cosines.

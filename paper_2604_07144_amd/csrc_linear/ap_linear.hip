@@ -1,6 +1,7 @@
 // C ABI of the operators on weights in 4 bits and of log probabilities: checks of arguments, choice of kernels and grids.
 #include <algorithm>
 
+#include "../csrc_attn/at_host.hpp"
 #include "li_few.hpp"
 #include "li_logprobs.hpp"
 #include "li_many.hpp"
@@ -8,11 +9,6 @@
 
 namespace {
 
-constexpr uint64_t kMost = 1ull << 31;              // rows, columns and blocks stay below
-constexpr uint64_t kMostGroups = 1ull << 24;        // and workgroups (of 256 threads: a grid holds less than 2^32)
-
-bool multiple(const void* p, uint64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-bool stride_ok(int64_t s, int64_t n) { return s >= 0 && s % n == 0; }
 uint32_t tiles_of(uint64_t n, uint64_t tile) { return (uint32_t)((n + tile - 1) / tile); }
 
 ap_status take_weights(const ap_weights* w, Weights* out) {
@@ -36,16 +32,6 @@ template <typename F> void for_group(uint32_t g, F f) {
     if (g == 32) f(std::integral_constant<uint32_t, 32>{});
     else if (g == 64) f(std::integral_constant<uint32_t, 64>{});
     else f(std::integral_constant<uint32_t, 128>{});
-}
-
-ap_status launched() { return hipGetLastError() == hipSuccess ? AP_OK : AP_ERR_DEVICE; }
-
-// magic and shift of a division of numbers below 2^31 by `d`: n / d = ((2 n) * magic >> 32) >> shift
-void divider(uint32_t d, uint32_t* magic, uint32_t* shift) {
-    uint32_t l = 0;
-    while ((1ull << l) < d) ++l;
-    *shift = l;
-    *magic = (uint32_t)(((1ull << (31 + l)) + d - 1) / d);
 }
 
 ap_status pack_params(const ap_weights* weights, const ap_vectors* values, PackParams* p, dim3* grid) {
@@ -94,7 +80,7 @@ ap_status linear_plan(const Weights& w, uint32_t n_tokens, uint32_t group, bool 
         for (const uint32_t tokens : {96u, 64u}) {
             if (tokens == 96 && group == 32) continue;
             const double step_us = kStepUs + kTileUs * (tokens / 16);
-            for (uint32_t n = 1; n <= 32 && n <= w.blocks; ++n) {
+            for (uint32_t n = 1; n == 1 || (n <= 32 && n <= w.blocks && sums < 256 * kMostGroups); ++n) {
                 const uint64_t rounds = ((uint64_t)r.n_outs * tiles_of(n_tokens, tokens) * n + kCus - 1) / kCus;
                 const double us = rounds * (tiles_of(w.blocks, n) * step_us + kEnterUs) + (n > 1 ? kJoinUs + 8.0 * n * sums / kPartBytesPerUs : 0.0);
                 if (least < 0 || us < least) least = us, parts = n, r.tokens = tokens;

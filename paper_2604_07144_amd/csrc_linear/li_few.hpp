@@ -34,8 +34,12 @@ template <uint32_t G, uint32_t T, bool kGated> struct FewShape {
     static constexpr uint32_t kSumLanes = T < 16 ? T * 4 : kLanes;                                  // that have tokens
     static constexpr bool kOneTile = T > 16;                                                        // a workgroup has one tile of outputs, not several
     static constexpr uint32_t kSums = kWaves * kTiles * kSumLanes * 16, kApart = kOneTile ? 0 : kSums;   // in the ring, or beside it
-    static constexpr uint32_t kFit = (160 * 1024 - kApart) / kStage, kRing = kFit < 8 ? kFit : 8;
-    static constexpr uint32_t kLds = kApart + (kRing * kStage > kSums ? kRing * kStage : kSums);
+    // X of a tile is taken by one of the wavefronts that share x where that spares more than the barrier it needs: [deep][group][token].  Gated,
+    // 64 tokens, 14336 outputs of 4096 inputs, each its own / shared: groups of 128 38 / 35 us, of 32 (8192 inputs) 80 / 91; 32 tokens 29 / 30.
+    static constexpr bool kShareX = kTiles == 4 && G == 128;
+    static constexpr uint32_t kXSums = kShareX ? kDeep * kWords * kTiles * 64 : 0;
+    static constexpr uint32_t kFit = (160 * 1024 - kApart - kXSums) / kStage, kRing = kFit < 8 ? kFit : 8;
+    static constexpr uint32_t kLds = kApart + kXSums + (kRing * kStage > kSums ? kRing * kStage : kSums);
 };
 
 // The wait for all but the `keep` newest steps of loads of `kLoads` each.
@@ -124,25 +128,46 @@ __global__ __launch_bounds__((FewShape<G, T, kGated>::kWaves * kLanes)) void k_l
     };
     const Unpack<E> unpack;
     f32x4 acc[TT] = {};
+    float* const x_sums = reinterpret_cast<float*>(lds + Shape::kLds - Shape::kXSums);
     auto add = [&] {
         const char* const at = lds + use;
         const char* const at_x = at + deep * Shape::kXBytes;
         const u32x4 c = *reinterpret_cast<const u32x4*>(at + Shape::kX + wave * 1024 + slot);
         const PairWords<G> pr = *reinterpret_cast<const PairWords<G>*>(at + Shape::kX + Shape::kCodes + wave * Shape::kPairLoads * 256 + col * kWords * 4);
+        float* const sums = x_sums + deep * (kGroups * TT * 16) + q * 4;
+        const uint32_t one = kOnes<E>;
+        const u32x4 all_ones = {one, one, one, one};
+        if constexpr (Shape::kShareX) {
+            if (aside < TT) {
+#pragma unroll
+                for (uint32_t g = 0; g < kGroups; ++g) {
+                    f32x4 ones = {};
+#pragma unroll
+                    for (uint32_t m = g * kSteps; m < (g + 1) * kSteps; ++m)
+                        ones = mfma16<E>(*reinterpret_cast<const u32x4*>(at_x + aside * 4096 + m / 2 * 2048 + x_slot[m % 2]), all_ones, ones);
+                    if (col == 0) *reinterpret_cast<f32x4*>(sums + (g * TT + aside) * 16) = ones;
+                }
+            }
+        }
 #pragma unroll
         for (uint32_t g = 0; g < kGroups; ++g) {
             f32x4 ones[TT] = {}, s[TT] = {};
-            const uint32_t one = kOnes<E>;
 #pragma unroll
             for (uint32_t m = g * kSteps; m < (g + 1) * kSteps; ++m) {
                 u32x4 a[TT];
 #pragma unroll
                 for (uint32_t i = 0; i < TT; ++i) a[i] = *reinterpret_cast<const u32x4*>(at_x + (T < 16 ? m * (kRows * 64) : i * 4096 + m / 2 * 2048) + x_slot[m % 2]);
+                if constexpr (!Shape::kShareX)
 #pragma unroll
-                for (uint32_t i = 0; i < TT; ++i) ones[i] = mfma16<E>(a[i], u32x4{one, one, one, one}, ones[i]);
+                    for (uint32_t i = 0; i < TT; ++i) ones[i] = mfma16<E>(a[i], all_ones, ones[i]);
                 const u32x4 v = unpack(c[m]);
 #pragma unroll
                 for (uint32_t i = 0; i < TT; ++i) s[i] = mfma16<E>(a[i], v, s[i]);
+            }
+            if constexpr (Shape::kShareX) {
+                if (g == 0) __syncthreads();
+#pragma unroll
+                for (uint32_t i = 0; i < TT; ++i) ones[i] = *reinterpret_cast<const f32x4*>(sums + (g * TT + i) * 16);
             }
             const float step = low16<E>(pr[g]), low = fmaf(-16.0f, step, high16<E>(pr[g]));
 #pragma unroll
@@ -188,6 +213,7 @@ __global__ __launch_bounds__((FewShape<G, T, kGated>::kWaves * kLanes)) void k_l
         arrived();
         if (i + kRing - 1 < all) load();
         if (begin + use_step * kDeep + deep < end) add();
+        else if constexpr (Shape::kShareX) __syncthreads();                                  // the one in add
         use = use == (kRing - 1) * Shape::kStage ? 0 : use + Shape::kStage;
         use_step = use_step + 1 == steps ? 0 : use_step + 1;
         if (--use_left == 0) leave();
