@@ -48,7 +48,7 @@ ap_status pack_params(const ap_weights* weights, const ap_vectors* values, PackP
 }
 
 struct LinearPlan {
-    bool many;
+    bool many, held;
     uint32_t tokens;                                // of a workgroup
     uint32_t part_blocks, n_parts;
     uint32_t n_outs, n_tokens;                      // workgroups over the outputs and tokens
@@ -96,6 +96,10 @@ ap_status linear_plan(const Weights& w, uint32_t n_tokens, uint32_t group, bool 
         // several tiles one after another, and no more workgroups are started than there are CUs.
         parts = std::max<uint32_t>(1, std::min(kCus / std::min(kCus, r.n_outs), w.blocks * aside / 64));
         if (r.tokens <= 16) r.n_outs = std::min(r.n_outs, kCus);
+        // From three tiles on x is brought to LDS once, where it fits, and not with each.  Brought with each / once, us: gated 14336 of 4096, 1, 4
+        // and 8 tokens 20.3 / 18.4, 20.2 / 18.2, 23.5 / 21.4; 128256 of 4096, 8 tokens 85 / 74; two tiles (6144 of 4096), 1 and 8 tokens 6.6 / 7.1
+        // and 7.6 / 7.4; one tile (4096 of 4096) 4.8 / 5.4 and 5.4 / 5.7.
+        r.held = r.tokens <= 8 && (uint64_t)tiles_of(w.blocks, parts) * r.tokens * 256 <= kHeldBytes && tiles > 2ull * kCus * aside;
     }
     r.part_blocks = tiles_of(w.blocks, parts), r.n_parts = tiles_of(w.blocks, r.part_blocks);
     if ((uint64_t)r.n_outs * r.n_tokens * r.n_parts >= kMostGroups / 4) return AP_ERR_RANGE;
@@ -124,7 +128,11 @@ ap_status run_linear(LinearParams p, const LinearPlan& plan, uint32_t dtype, uin
                         return;
                     }
                     for_one_of<4, 8, 16, 32, 64>(plan.tokens, [&](auto t) {
-                        hipLaunchKernelGGL((k_linear_few<E, g(), t(), gates(), whole()>), dim3(plan.n_outs, 1, plan.n_parts), dim3(FewShape<g(), t(), gates()>::kWaves * kLanes), 0, on, p);
+                        for_truth(plan.held, [&](auto held) {
+                            if constexpr (!held() || t() <= 8)
+                                hipLaunchKernelGGL((k_linear_few<E, g(), t(), gates(), held(), whole()>), dim3(plan.n_outs, 1, plan.n_parts),
+                                                   dim3(FewShape<g(), t(), gates(), held()>::kWaves * kLanes), 0, on, p);
+                        });
                     });
                 });
             });

@@ -22,18 +22,19 @@ namespace {
 
 template <typename E> constexpr uint32_t kOnes = std::is_same_v<E, bf16> ? 0x3F803F80u : 0x3C003C00u;
 
-// Of a kernel for up to T tokens.
-template <uint32_t G, uint32_t T, bool kGated> struct FewShape {
-    static constexpr uint32_t kWaves = T == 8 || T == 16 ? 8 : 16, kTiles = T <= 16 ? 1 : T / 16, kAside = T <= 16 ? (kGated ? 2 : 1) : T / 8;
+// Of a kernel for up to T tokens.  kHeld: all of x is brought to LDS first, and stays; there is room for kHeldBytes of it.
+constexpr uint32_t kHeldBytes = 64 * 1024;
+template <uint32_t G, uint32_t T, bool kGated, bool kHeld> struct FewShape {
+    static constexpr uint32_t kWaves = !kHeld && (T == 8 || T == 16) ? 8 : 16, kTiles = T <= 16 ? 1 : T / 16, kAside = T <= 16 ? (kGated ? 2 : 1) : T / 8;
     static constexpr uint32_t kDeep = kWaves / kAside, kOuts = kGated ? kAside / 2 : kAside;     // kOuts: tiles of 16 outputs side by side
     static constexpr uint32_t kWords = kBlock / G, kPairLoads = (16 * kWords + kLanes - 1) / kLanes;
     // x of a step and deep index: kTiles times 4 KiB, or of fewer than 16 tokens as many rows of 256 bytes; in loads of 1 KiB
-    static constexpr uint32_t kRows = T < 16 ? T : 16, kXBytes = kTiles * kRows * 256, kXLoads = (kXBytes / 1024 + kAside - 1) / kAside;
+    static constexpr uint32_t kRows = T < 16 ? T : 16, kXBytes = kTiles * kRows * 256, kXLoads = kHeld ? 0 : (kXBytes / 1024 + kAside - 1) / kAside;
     static constexpr uint32_t kLoads = 1 + kPairLoads + kXLoads;                                    // of a wavefront and step
-    static constexpr uint32_t kX = kDeep * kXBytes, kCodes = kWaves * 1024, kPairs = kWaves * kPairLoads * 256, kStage = kX + kCodes + kPairs;
+    static constexpr uint32_t kX = kHeld ? 0 : kDeep * kXBytes, kCodes = kWaves * 1024, kPairs = kWaves * kPairLoads * 256, kStage = kX + kCodes + kPairs;
     static constexpr uint32_t kSumLanes = T < 16 ? T * 4 : kLanes;                                  // that have tokens
     static constexpr bool kOneTile = T > 16;                                                        // a workgroup has one tile of outputs, not several
-    static constexpr uint32_t kSums = kWaves * kTiles * kSumLanes * 16, kApart = kOneTile ? 0 : kSums;   // in the ring, or beside it
+    static constexpr uint32_t kSums = kWaves * kTiles * kSumLanes * 16, kApart = (kOneTile ? 0 : kSums) + (kHeld ? kHeldBytes : 0);   // in the ring, or beside it
     // X of a tile is taken by one of the wavefronts that share x where that spares more than the barrier it needs: [deep][group][token].  Gated,
     // 64 tokens, 14336 outputs of 4096 inputs, each its own / shared: groups of 128 38 / 35 us, of 32 (8192 inputs) 80 / 91; 32 tokens 29 / 30.
     static constexpr bool kShareX = kTiles == 4 && G == 128;
@@ -50,9 +51,9 @@ template <uint32_t kLoads, uint32_t kMost> __device__ __forceinline__ void wait_
     wait_loads<kLoads * kMost>();
 }
 
-template <typename E, uint32_t G, uint32_t T, bool kGated, bool kWhole>
-__global__ __launch_bounds__((FewShape<G, T, kGated>::kWaves * kLanes)) void k_linear_few(const LinearParams p) {
-    using Shape = FewShape<G, T, kGated>;
+template <typename E, uint32_t G, uint32_t T, bool kGated, bool kHeld, bool kWhole>
+__global__ __launch_bounds__((FewShape<G, T, kGated, kHeld>::kWaves * kLanes)) void k_linear_few(const LinearParams p) {
+    using Shape = FewShape<G, T, kGated, kHeld>;
     constexpr uint32_t TT = Shape::kTiles, kAside = Shape::kAside, kDeep = Shape::kDeep, kOuts = Shape::kOuts, kGroups = kBlock / G, kSteps = G / 32;
     constexpr uint32_t kRing = Shape::kRing, kWords = Shape::kWords, kRows = Shape::kRows;
     __shared__ __attribute__((aligned(16))) char lds[Shape::kLds];
@@ -87,8 +88,8 @@ __global__ __launch_bounds__((FewShape<G, T, kGated>::kWaves * kLanes)) void k_l
     enter();
     // x: rows of 64 (fewer than 16 tokens) or 128 bytes, kRows of them for each 32 or 64 columns of a tile
     constexpr uint32_t kRowLanes = T < 16 ? 4 : 8;
-    const char* x[Shape::kXLoads];
-    uint32_t x_col[Shape::kXLoads];                        // first column of a lane's piece in the block
+    const char* x[Shape::kXLoads + 1];
+    uint32_t x_col[Shape::kXLoads + 1];                    // first column of a lane's piece in the block
     uint32_t x_slot[2];                                    // where the lane's operand of 32 columns lies, in those, of even and odd ones
 #pragma unroll
     for (uint32_t j = 0; j < Shape::kXLoads; ++j) {
@@ -109,6 +110,17 @@ __global__ __launch_bounds__((FewShape<G, T, kGated>::kWaves * kLanes)) void k_l
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)lds;
     const uint32_t base_x = base + deep * Shape::kXBytes + aside * Shape::kXLoads * 1024 % Shape::kXBytes, base_codes = base + Shape::kX + wave * 1024,
                    base_pairs = base + Shape::kX + Shape::kCodes + wave * Shape::kPairLoads * 256;
+    const uint32_t held = base + Shape::kLds - kHeldBytes;
+    if constexpr (kHeld) {                                 // [block] as a step's
+        static_assert(T < 16);
+        const uint32_t pieces = (end - begin) * kRows * 16;
+        for (uint32_t e0 = wave * kLanes; e0 < pieces; e0 += Shape::kWaves * kLanes) {
+            const uint32_t e = min(e0 + lane, pieces - 1), b = begin + e / (kRows * 16), in = e % (kRows * 16), row = in / 4 % kRows;
+            const uint32_t c = b * kBlock + in / 4 / kRows * 32 + turned(row, in % 4) * 8;
+            const bool there = kWhole || c < p.w[0].n_in;
+            load_to_lds<0>(there ? p.x + (int64_t)min(row, p.n_tokens - 1) * p.x_stride + 2ull * c : (const char*)&kZeros, held + e0 * 16);
+        }
+    }
     auto load = [&] {
         const uint32_t b = min(begin + load_step * kDeep + deep, end - 1);                  // behind the last block: the last one, not added
         load_to_lds<0>(codes + (uint64_t)b * 64, base_codes + fill);
@@ -126,12 +138,13 @@ __global__ __launch_bounds__((FewShape<G, T, kGated>::kWaves * kLanes)) void k_l
             if (++load_tile < tiles) enter();
         }
     };
+    uint32_t use_step = first_step;
     const Unpack<E> unpack;
     f32x4 acc[TT] = {};
-    float* const x_sums = reinterpret_cast<float*>(lds + Shape::kLds - Shape::kXSums);
+    float* const x_sums = reinterpret_cast<float*>(lds + Shape::kLds - Shape::kXSums - (kHeld ? kHeldBytes : 0));
     auto add = [&] {
         const char* const at = lds + use;
-        const char* const at_x = at + deep * Shape::kXBytes;
+        const char* const at_x = kHeld ? lds + (Shape::kLds - kHeldBytes) + (use_step * kDeep + deep) * Shape::kXBytes : at + deep * Shape::kXBytes;
         const u32x4 c = *reinterpret_cast<const u32x4*>(at + Shape::kX + wave * 1024 + slot);
         const PairWords<G> pr = *reinterpret_cast<const PairWords<G>*>(at + Shape::kX + Shape::kCodes + wave * Shape::kPairLoads * 256 + col * kWords * 4);
         float* const sums = x_sums + deep * (kGroups * TT * 16) + q * 4;
@@ -176,7 +189,7 @@ __global__ __launch_bounds__((FewShape<G, T, kGated>::kWaves * kLanes)) void k_l
                 for (uint32_t j = 0; j < 4; ++j) acc[i][j] = fmaf(step, s[i][j], fmaf(low, ones[i][j], acc[i][j]));
         }
     };
-    uint32_t use_step = first_step, use_left = steps, use_tile = 0;
+    uint32_t use_left = steps, use_tile = 0;
     auto leave = [&] {                                     // a tile is done: its sums meet, and each thread finishes single outputs
         constexpr uint32_t kWide = Shape::kSumLanes, kTile = kWide * 4;
         float* const sums = reinterpret_cast<float*>(lds + (Shape::kOneTile ? 0 : kRing * Shape::kStage));          // [wavefront][tile][lane][4]
@@ -203,11 +216,15 @@ __global__ __launch_bounds__((FewShape<G, T, kGated>::kWaves * kLanes)) void k_l
         use_left = steps, ++use_tile;
     };
     auto arrived = [&] {
-        if constexpr (kAside > 1) __syncthreads();
+        if constexpr (kAside > 1 && !kHeld) __syncthreads();
         else wait_lds();                                   // what is loaded next comes to where the last step was read
     };
     const uint32_t all = tiles * steps;
     for (uint32_t i = 0; i < min(all, kRing - 1); ++i) load();
+    if constexpr (kHeld) {                                 // x was first: what came after it may still be on its way
+        wait_steps<Shape::kLoads, kRing - 1>(min(all, kRing - 1));
+        __syncthreads();
+    }
     for (uint32_t i = 0; i < all; ++i) {
         wait_steps<Shape::kLoads, kRing - 2>(min(all - 1 - i, kRing - 2));
         arrived();

@@ -197,3 +197,19 @@ def test_far_rows():
     y = wide[:, 512:532]
     m.linear(wide[:, :256], y=y)
     check_linear(m, x, y)
+
+
+@pytest.mark.parametrize("tokens", [1, 4, 5, 8])
+@pytest.mark.parametrize("n_in,group,dtype", [(256, 128, "bf16"), (1096, 32, "fp16"), (2056, 64, "bf16")])
+def test_outputs_in_several_tiles(tokens, n_in, group, dtype):
+    """So many outputs that a workgroup has several tiles of them, of which the last is not full."""
+    m = Matrix(256 * 48 + 77, n_in, group, dtype, seed=tokens)
+    x = rows(tokens, n_in, dtype, seed=n_in, apart=8)
+    check_linear(m, x, m.linear(x))
+
+
+@pytest.mark.parametrize("tokens", [3, 8, 16])
+def test_gated_in_several_tiles(tokens):
+    gate, up = (Matrix(256 * 33 + 5, 520, 64, "bf16", seed=90 + i) for i in range(2))
+    x = rows(tokens, 520, "bf16", seed=92)
+    check_gated(gate, up, x, gated(gate, up, x), "silu")
