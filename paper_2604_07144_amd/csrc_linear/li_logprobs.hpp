@@ -95,8 +95,8 @@ template <uint32_t M = kLanes / 2> __device__ __forceinline__ uint64_t settled(u
     else return key;
 }
 // Any keys in rising order over the lanes.
-template <uint32_t N = 2, uint32_t M = 1> __device__ __forceinline__ uint64_t rising(uint64_t key, uint32_t lane) {
-    const uint64_t other = across<M>(key);
+template <uint32_t N = 2, uint32_t M = 1, typename K> __device__ __forceinline__ K rising(K key, uint32_t lane) {
+    const K other = across<M>(key);
     const bool up = (lane & N) == 0 || N == kLanes;
     key = ((lane & M) != 0) == up ? max(key, other) : min(key, other);
     if constexpr (M > 1) return rising<N, M / 2>(key, lane);
@@ -200,7 +200,7 @@ template <typename E> __global__ __launch_bounds__(kLogThreads) void k_logprobs(
         if (p.top && __any(largest > least)) {
             if (!begun) {
                 // Of the lanes' largest entries the one in the last place that is asked for: below it lies no alternative.
-                const uint32_t last = (uint32_t)(of_lane(rising((uint64_t)order_of(largest) << 32, lane), kLanes - p.top) >> 32);
+                const uint32_t last = (uint32_t)__builtin_amdgcn_readlane(rising(order_of(largest), lane), kLanes - p.top);
                 if (from_order(last) > -INFINITY) least = from_order(last - (last == 0x80000000u ? 2 : 1));   // zero is two numbers
                 begun = true;
             }

@@ -117,12 +117,9 @@ def test_captured():
         assert torch.equal(words, want) and (back - x).abs().max() < 0.5
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
-@pytest.mark.parametrize("scale", [1e-30, 1e-4, 1.0, 1e4, 1e30])
+@pytest.mark.parametrize("dtype,scale", [("bf16", 1e-30), ("bf16", 1e-4), ("bf16", 1.0), ("bf16", 1e30), ("fp16", 1e-4), ("fp16", 1.0), ("fp16", 1e3)])
 def test_values_of_any_size(dtype, scale):
     """Steps from next to nothing to next to overflow, and values that lie in the middle between two codes."""
-    if dtype == "fp16" and not 1e-4 <= scale <= 1e3:
-        pytest.skip("beyond the type's range")
     gen = torch.Generator(device="cuda")
     gen.manual_seed(7)
     x = (scale * torch.randn((64, 512), generator=gen, device="cuda")).to(TYPES[dtype][0])
