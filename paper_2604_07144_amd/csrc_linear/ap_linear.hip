@@ -73,12 +73,13 @@ ap_status linear_plan(const Weights& w, uint32_t n_tokens, uint32_t group, bool 
     r.many = n_tokens > kMostFew;
     uint32_t parts = 1;
     if (r.many) {
-        // Tiles of 64 or 96 tokens (64 for small groups, whose sums leave fewer registers), and the inputs in as many parts, as the estimate
-        // likes best: little in the tiles that is no token, workgroups that fill the chip in whole rounds, few parts to write and read.
+        // Tiles of 64, 96 or 112 tokens (small groups, whose pairs and sums leave fewer registers, up to 64 and 96), and the inputs in as many
+        // parts, as the estimate likes best: little in the tiles that is no token, workgroups that fill the chip in whole rounds, few parts
+        // to write and read.
         r.n_outs = tiles_of(tiles, kManyTiles * kManyWaves);
         double least = -1;
-        for (const uint32_t tokens : {96u, 64u}) {
-            if (tokens == 96 && group == 32) continue;
+        for (const uint32_t tokens : {112u, 96u, 64u}) {
+            if (tokens > (group == 32 ? 64 : group == 64 ? 96 : 112)) continue;
             const double step_us = kStepUs + kTileUs * (tokens / 16);
             for (uint32_t n = 1; n == 1 || (n <= 32 && n <= w.blocks && sums < 256 * kMostGroups); ++n) {
                 const uint64_t rounds = ((uint64_t)r.n_outs * tiles_of(n_tokens, tokens) * n + kCus - 1) / kCus;
@@ -124,7 +125,8 @@ ap_status run_linear(LinearParams p, const LinearPlan& plan, uint32_t dtype, uin
                                                on, p, plan.n_outs, plan.n_tokens);
                         };
                         if (plan.tokens == 64) go(std::integral_constant<uint32_t, 4>{});
-                        else if constexpr (g() != 32) go(std::integral_constant<uint32_t, 6>{});
+                        else if constexpr (g() == 64) go(std::integral_constant<uint32_t, 6>{});
+                        else if constexpr (g() == 128) plan.tokens == 96 ? go(std::integral_constant<uint32_t, 6>{}) : go(std::integral_constant<uint32_t, 7>{});
                         return;
                     }
                     for_one_of<4, 8, 16, 32, 64>(plan.tokens, [&](auto t) {

@@ -17,7 +17,7 @@ template <uint32_t G, uint32_t TT> struct ManyShape {
     static constexpr uint32_t kWords = kBlock / G, kPairLoads = kWords;                     // 64 rows of so many words
     static constexpr uint32_t kX = TT * 4096, kCodes = kManyWaves * kManyTiles * 1024, kPairs = kManyWaves * kPairLoads * 256;
     static constexpr uint32_t kStage = kX + kCodes + kPairs, kLds = 2 * kStage + kWords * TT * 64;
-    static constexpr uint32_t kXLoads = TT / 2;                                             // of a wavefront
+    static constexpr uint32_t kXLoads = (TT + 1) / 2;                                       // of a wavefront; the last may have fewer
 };
 
 template <typename E, uint32_t G, uint32_t TT, bool kGated, bool kWhole>
@@ -69,6 +69,7 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
 #pragma unroll
         for (uint32_t j = 0; j < Shape::kXLoads; ++j) {
             const uint32_t f = wave * Shape::kXLoads + j;
+            if (TT % 2 && f >= TT * 4) break;
             const bool in = kWhole || b * kBlock + f % 4 * 32 + lpiece * 8 < p.w[0].n_in;
             load_to_lds<0>(in ? x[j] : (const char*)&kZeros, to + f * 1024);
             x[j] += 256;
@@ -106,7 +107,6 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
 #pragma unroll
             for (uint32_t g = 0; g < kWords; ++g) step[r][g] = low16<E>(pr[g]), low[r][g] = fmaf(-16.0f, step[r][g], high16<E>(pr[g]));
         }
-        __syncthreads();
 #pragma unroll
         for (uint32_t i = 0; i < TT; ++i) {
             u32x4 a[4];
@@ -114,12 +114,13 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
             for (uint32_t m = 0; m < 4; ++m) a[m] = *reinterpret_cast<const u32x4*>(in + (i * 4 + m) * 1024 + slot);
 #pragma unroll
             for (uint32_t g = 0; g < kWords; ++g) {
-                const f32x4 xs = *reinterpret_cast<const f32x4*>(sums + g * (TT * 16) + i * 16 + q * 4);
                 f32x4 s[R] = {};
 #pragma unroll
                 for (uint32_t m = g * kSteps; m < (g + 1) * kSteps; ++m)
 #pragma unroll
                     for (uint32_t r = 0; r < R; ++r) s[r] = mfma16<E>(a[m], w[r][m], s[r]);
+                if (i == 0 && g == 0) __syncthreads();                                      // X is there; codes are unpacked beside the first products
+                const f32x4 xs = *reinterpret_cast<const f32x4*>(sums + g * (TT * 16) + i * 16 + q * 4);
 #pragma unroll
                 for (uint32_t r = 0; r < R; ++r)
 #pragma unroll
