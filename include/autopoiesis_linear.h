@@ -39,7 +39,7 @@ extern "C" {
  *   pairs : row r at pairs + r * pair_stride: for each `group` (32, 64 or 128) columns of the blocks a pair (step, lo) of the
  *           16-bit type `dtype`.  Address and stride are multiples of a block's bytes, 512 / group.
  * A code stands for lo + step * code.  Columns from n_in on stand for nothing, but pairs of groups that have no other column have to
- * be numbers (ap_weights_pack makes them zero). */
+ * be numbers (ap_weights_pack makes them zero).  n_out, n_in and n_out * blocks are below 2^31. */
 typedef struct {
     uint32_t dtype, group, n_out, n_in;
     void *codes, *pairs;
@@ -64,7 +64,9 @@ ap_status ap_weights_read(const ap_weights *weights, const ap_vectors *values, v
 /* y = x W^T (+ add) for n_tokens rows: y[t][n] = add[t][n] + sum_k x[t][k] (lo + step * code)[n][k], in 32 bits with each
  * rounded once, at its end.  x (16-byte aligned) has n_in columns, y and add have n_out; all are of the weights' type.  add may
  * be NULL, or y itself; with a stride of 0 it is a bias.  y must not overlap x.  Rows are apart: what is not a number in one
- * of x reaches only the same row of y. */
+ * of x reaches only the same row of y.  No weight is rounded: sums over a group's columns of x (16 + code) and of x meet
+ * step and lo - 16 step in 32 bits.  Where such a sum or product passes 32 bits (x and weights of 2^120 and more) or x holds an
+ * infinity the row can be NaN. */
 ap_status ap_linear_workspace(const ap_weights *weights, uint32_t n_tokens, uint64_t *bytes);
 ap_status ap_linear(const ap_weights *weights, const ap_vectors *x, const ap_vectors *add, const ap_vectors *y, uint32_t n_tokens,
                     void *workspace, uint64_t workspace_bytes, void *stream);
@@ -83,7 +85,7 @@ typedef struct {
     int64_t stride;
 } ap_logits;
 
-/* With p = e^s / sum e^s over s = scale * logits (scale > 0: one over the temperature), of each row:
+/* With p = e^s / sum e^s over s = scale * logits (scale > 0, one over the temperature; log2(e) times it is finite), of each row:
  *   logprob     : log p of tokens[row], 0 where that is outside [0, vocab); tokens may be NULL, then logprob is too.
  *   entropy     : - sum p log p; may be NULL.
  *   top_id, top_logprob : [n_rows][top], the `top` (at most 64) tokens of the largest logits, of equal ones the lowest token

@@ -8,6 +8,10 @@
 // Alternatives: a wavefront holds its 64 largest logits in order, one a lane, as whole numbers (value, then lowest token), and
 // looks only at entries above the last place that is asked for.  Those are gathered in LDS and merged in when there are many.
 // Wavefronts of a row, and pieces of a row where there are few rows, are joined in order at the end.
+//
+// Measured, 128256 tokens, us: 2311 rows in bf16 with 8 alternatives 135 (4.4 TB/s; a copy 5.1), with none 117; 64 rows in 32 bits with 20 alternatives
+// 22, 8 rows in bf16 with 5 13.5: a launch that joins (5) and finding the alternatives (64 rows without any 10.5), which is vector work
+// of every wavefront, sorting networks of 64 keys.
 #ifndef LI_LOGPROBS_HPP
 #define LI_LOGPROBS_HPP
 

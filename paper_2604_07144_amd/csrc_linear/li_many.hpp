@@ -4,6 +4,11 @@
 // outputs, four tiles of 16 each, so an operand of x that is read from LDS meets four of weights, and codes are unpacked once for
 // all tokens.  Blocks of 128 columns follow one another; the next one is on its way to the other half of LDS while the present
 // one is worked on.  The sums X of x, which all outputs share, are taken by a wavefront for each tile of tokens.
+//
+// A tile of 16 tokens and 64 outputs is 16 products (256 cycles) and 32 multiply-adds that scale them, which the compiler puts between the
+// next tile's products.  Measured, gated 14336 outputs of 4096 inputs, bf16, TFLOP/s (a large product of the library 1130): 4999 tokens
+// 1010 with groups of 128; 2048 tokens 880 with groups of 128, 730 of 64, 555 of 32, which scale two and four times as often.  Without the
+// loads 20 % less time, without the scaling 4 %; weights two blocks ahead in a ring of three changed nothing.
 #ifndef LI_MANY_HPP
 #define LI_MANY_HPP
 

@@ -213,3 +213,19 @@ def test_gated_in_several_tiles(tokens):
     gate, up = (Matrix(256 * 33 + 5, 520, 64, "bf16", seed=90 + i) for i in range(2))
     x = rows(tokens, 520, "bf16", seed=92)
     check_gated(gate, up, x, gated(gate, up, x), "silu")
+
+
+@pytest.mark.parametrize("tokens", [96, 97, 112, 113, 192, 193, 224, 225, 336, 337])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_tiles_of_tokens(tokens, group):
+    """Just full and just overfull tiles of the kernel of many rows."""
+    m = Matrix(530, 256, group, "fp16", seed=tokens)
+    x = rows(tokens, 256, "fp16", seed=tokens)
+    check_linear(m, x, m.linear(x))
+
+
+@pytest.mark.parametrize("tokens", [120, 3000])
+def test_more_outputs_than_one_tile_has_with_many_rows(tokens):
+    gate, up = (Matrix(600, 384, 128, "bf16", seed=95 + i) for i in range(2))
+    x = rows(tokens, 384, "bf16", seed=97)
+    check_gated(gate, up, x, gated(gate, up, x), "silu")
