@@ -79,6 +79,9 @@ template <typename E> __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, 
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(Vec8<fp16>, a), __builtin_bit_cast(Vec8<fp16>, b), c, 0, 0, 0);
 }
 
+// c += a b of 16 x 4 and 4 x 16 numbers in 32 bits: a lane has row (column) lane % 16 and place lane / 16 of the sum.
+__device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
 // The number of lane ^ M.
 template <uint32_t M> __device__ __forceinline__ uint32_t across(uint32_t x) {
     if constexpr (M == 1) return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true);              // quads 1 0 3 2

@@ -27,6 +27,13 @@ namespace {
 
 template <typename E> constexpr uint32_t kOnes = std::is_same_v<E, bf16> ? 0x3F803F80u : 0x3C003C00u;
 
+// c with the sums over 32 columns of x added, in the lanes that have group g: c[0] is of group lane / 16 and token lane % 16.  (Ones in the rows of
+// those lanes only; x is the other operand here.)
+template <typename E> __device__ __forceinline__ f32x4 sum_of_group(uint32_t g, u32x4 x, uint32_t col, f32x4 c) {
+    const uint32_t one = col / 4 == g ? kOnes<E> : 0;
+    return mfma16<E>(u32x4{one, one, one, one}, x, c);
+}
+
 // Of a kernel for up to T tokens.  kHeld: all of x is brought to LDS first, and stays; there is room for kHeldBytes of it.
 constexpr uint32_t kHeldBytes = 64 * 1024;
 template <uint32_t G, uint32_t T, bool kGated, bool kHeld> struct FewShape {
@@ -40,10 +47,13 @@ template <uint32_t G, uint32_t T, bool kGated, bool kHeld> struct FewShape {
     static constexpr uint32_t kSumLanes = T < 16 ? T * 4 : kLanes;                                  // that have tokens
     static constexpr bool kOneTile = T > 16;                                                        // a workgroup has one tile of outputs, not several
     static constexpr uint32_t kSums = kWaves * kTiles * kSumLanes * 16, kApart = (kOneTile ? 0 : kSums) + (kHeld ? kHeldBytes : 0);   // in the ring, or beside it
-    // X of a tile is taken by one of the wavefronts that share x where that spares more than the barrier it needs: [deep][group][token].  Gated,
-    // 64 tokens, 14336 outputs of 4096 inputs, each its own / shared: groups of 128 38 / 35 us, of 32 (8192 inputs) 80 / 91; 32 tokens 29 / 30.
-    static constexpr bool kShareX = kTiles == 4 && G == 128;
-    static constexpr uint32_t kXSums = kShareX ? kDeep * kWords * kTiles * 64 : 0;
+    // X of a tile of tokens is taken by one of the wavefronts that share x, where that spares more than the barrier it needs: [deep][group][token].
+    // Gated, 14336 outputs of 4096 inputs, groups of 128, each its own / shared: 64 tokens 38 / 35 us, 32 tokens 29 / 30.  Groups of 32 and 64
+    // have (lo - 16 step) X on the matrix units too, in 32 bits and four groups at once, which spares half of the multiply-adds; X is then
+    // [deep][tile][lane], of group lane / 16 and token lane % 16.  64 tokens, gated 14336 of 8192, groups of 32: 86 / 77 us; 14336 of 4096,
+    // groups of 64 40.4 / 38.3, of 128 35.7 / 38.6.
+    static constexpr bool kShareX = kTiles == 4, kLowByMatrix = kShareX && G <= 64;
+    static constexpr uint32_t kXSums = !kShareX ? 0 : kDeep * kTiles * (kLowByMatrix ? kLanes * 4 : kWords * 64);
     static constexpr uint32_t kFit = (160 * 1024 - kApart - kXSums) / kStage, kRing = kFit < 8 ? kFit : 8;
     static constexpr uint32_t kLds = kApart + kXSums + (kRing * kStage > kSums ? kRing * kStage : kSums);
 };
@@ -153,6 +163,36 @@ __global__ __launch_bounds__((FewShape<G, T, kGated, kHeld>::kWaves * kLanes)) v
         const u32x4 c = *reinterpret_cast<const u32x4*>(at + Shape::kX + wave * 1024 + slot);
         const PairWords<G> pr = *reinterpret_cast<const PairWords<G>*>(at + Shape::kX + Shape::kCodes + wave * Shape::kPairLoads * 256 + col * kWords * 4);
         float* const sums = x_sums + deep * (kGroups * TT * 16) + q * 4;
+        if constexpr (Shape::kLowByMatrix) {
+            float* const xs = x_sums + deep * (TT * kLanes) + lane;
+            if (aside < TT) {
+                f32x4 mine = {};
+#pragma unroll
+                for (uint32_t m = 0; m < 4; ++m) mine = sum_of_group<E>(m / kSteps, *reinterpret_cast<const u32x4*>(at_x + aside * 4096 + m / 2 * 2048 + x_slot[m % 2]), col, mine);
+                xs[aside * kLanes] = mine[0];
+            }
+#pragma unroll
+            for (uint32_t g = 0; g < kGroups; ++g) {
+                f32x4 s[TT] = {};
+#pragma unroll
+                for (uint32_t m = g * kSteps; m < (g + 1) * kSteps; ++m) {
+                    const u32x4 v = unpack(c[m]);
+#pragma unroll
+                    for (uint32_t i = 0; i < TT; ++i) s[i] = mfma16<E>(*reinterpret_cast<const u32x4*>(at_x + i * 4096 + m / 2 * 2048 + x_slot[m % 2]), v, s[i]);
+                }
+                const float step = low16<E>(pr[g]);
+#pragma unroll
+                for (uint32_t i = 0; i < TT; ++i)
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) acc[i][j] = fmaf(step, s[i][j], acc[i][j]);
+            }
+            __syncthreads();
+            const uint32_t word = *reinterpret_cast<const uint32_t*>(at + Shape::kX + Shape::kCodes + wave * Shape::kPairLoads * 256 + (col * kWords + q % kWords) * 4);
+            const float low = fmaf(-16.0f, low16<E>(word), high16<E>(word));
+#pragma unroll
+            for (uint32_t i = 0; i < TT; ++i) acc[i] = mfma4(xs[i * kLanes], low, acc[i]);
+            return;
+        }
         const uint32_t one = kOnes<E>;
         const u32x4 all_ones = {one, one, one, one};
         if constexpr (Shape::kShareX) {

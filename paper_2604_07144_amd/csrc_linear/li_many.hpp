@@ -7,7 +7,7 @@
 //
 // A tile of 16 tokens and 64 outputs is 16 products (256 cycles) and 32 multiply-adds that scale them, which the compiler puts between the
 // next tile's products.  Measured, gated 14336 outputs of 4096 inputs, bf16, TFLOP/s (a large product of the library 1130): 4999 tokens
-// 1010 with groups of 128; 2048 tokens 880 with groups of 128, 730 of 64, 555 of 32, which scale two and four times as often.  Without the
+// 1010 with groups of 128; 2048 tokens 880 with groups of 128, 745 of 64, 580 of 32, which scale two and four times as often.  Without the
 // loads 20 % less time, without the scaling 4 %; weights two blocks ahead in a ring of three changed nothing.
 #ifndef LI_MANY_HPP
 #define LI_MANY_HPP
@@ -22,6 +22,9 @@ template <uint32_t G, uint32_t TT> struct ManyShape {
     static constexpr uint32_t kWords = kBlock / G, kPairLoads = kWords;                     // 64 rows of so many words
     static constexpr uint32_t kX = TT * 4096, kCodes = kManyWaves * kManyTiles * 1024, kPairs = kManyWaves * kPairLoads * 256;
     static constexpr uint32_t kStage = kX + kCodes + kPairs, kLds = 2 * kStage + kWords * TT * 64;
+    // (lo - 16 step) X by a product in 32 bits, as in the kernel of few rows.  Gated 14336 of 4096, 2048 tokens, off / on: groups of 32 866 / 828 us,
+    // of 64 645 / 698.
+    static constexpr bool kLowByMatrix = G == 32;
     static constexpr uint32_t kXLoads = (TT + 1) / 2;                                       // of a wavefront; the last may have fewer
 };
 
@@ -82,7 +85,7 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
     };
     const Unpack<E> unpack;
     f32x4 acc[R][TT] = {};
-    float* const sums = reinterpret_cast<float*>(lds + 2 * Shape::kStage);                  // X: [group][token]
+    float* const sums = reinterpret_cast<float*>(lds + 2 * Shape::kStage);                  // X: [group][token], or [tile][lane]
     load(begin, 0);
     for (uint32_t b = begin; b < end; ++b) {
         const uint32_t half = (b - begin) % 2;
@@ -90,7 +93,14 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
         wait_loads<0>();
         __syncthreads();
         if (b + 1 < end) load(b + 1, half ^ 1);
-        if (wave < TT) {
+        if constexpr (Shape::kLowByMatrix) {
+            if (wave < TT) {
+                f32x4 s = {};
+#pragma unroll
+                for (uint32_t m = 0; m < 4; ++m) s = sum_of_group<E>(m, *reinterpret_cast<const u32x4*>(in + (wave * 4 + m) * 1024 + slot), col, s);
+                sums[wave * kLanes + lane] = s[0];
+            }
+        } else if (wave < TT) {
 #pragma unroll
             for (uint32_t g = 0; g < kWords; ++g) {
                 const uint32_t one = kOnes<E>;
@@ -102,7 +112,7 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
             }
         }
         u32x4 w[R][4];
-        float step[R][kWords], low[R][kWords];
+        float step[R][kWords], low[R][kWords], low4[R];
 #pragma unroll
         for (uint32_t r = 0; r < R; ++r) {
             const u32x4 c = *reinterpret_cast<const u32x4*>(in + Shape::kX + (wave * R + r) * 1024 + slot);
@@ -111,6 +121,10 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
             for (uint32_t m = 0; m < 4; ++m) w[r][m] = unpack(c[m]);
 #pragma unroll
             for (uint32_t g = 0; g < kWords; ++g) step[r][g] = low16<E>(pr[g]), low[r][g] = fmaf(-16.0f, step[r][g], high16<E>(pr[g]));
+            if constexpr (Shape::kLowByMatrix) {
+                const uint32_t word = *reinterpret_cast<const uint32_t*>(in + Shape::kX + Shape::kCodes + wave * Shape::kPairLoads * 256 + ((r * 16 + col) * kWords + q) * 4);
+                low4[r] = fmaf(-16.0f, low16<E>(word), high16<E>(word));
+            }
         }
 #pragma unroll
         for (uint32_t i = 0; i < TT; ++i) {
@@ -125,6 +139,18 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
 #pragma unroll
                     for (uint32_t r = 0; r < R; ++r) s[r] = mfma16<E>(a[m], w[r][m], s[r]);
                 if (i == 0 && g == 0) __syncthreads();                                      // X is there; codes are unpacked beside the first products
+                if constexpr (Shape::kLowByMatrix) {
+#pragma unroll
+                    for (uint32_t r = 0; r < R; ++r)
+#pragma unroll
+                        for (uint32_t j = 0; j < 4; ++j) acc[r][i][j] = fmaf(step[r][g], s[r][j], acc[r][i][j]);
+                    if (g + 1 == kWords) {
+                        const float xs = sums[i * kLanes + lane];
+#pragma unroll
+                        for (uint32_t r = 0; r < R; ++r) acc[r][i] = mfma4(xs, low4[r], acc[r][i]);
+                    }
+                    continue;
+                }
                 const f32x4 xs = *reinterpret_cast<const f32x4*>(sums + g * (TT * 16) + i * 16 + q * 4);
 #pragma unroll
                 for (uint32_t r = 0; r < R; ++r)
