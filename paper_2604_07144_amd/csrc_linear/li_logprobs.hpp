@@ -9,9 +9,10 @@
 // looks only at entries above the last place that is asked for.  Those are gathered in LDS and merged in when there are many.
 // Wavefronts of a row, and pieces of a row where there are few rows, are joined in order at the end.
 //
-// Measured, 128256 tokens, us: 2311 rows in bf16 with 8 alternatives 135 (4.4 TB/s; a copy 5.1), with none 117; 64 rows in 32 bits with 20 alternatives
-// 22, 8 rows in bf16 with 5 13.5: a launch that joins (5) and finding the alternatives (64 rows without any 10.5), which is vector work
-// of every wavefront, sorting networks of 64 keys.
+// Measured, 128256 tokens, us: 2311 rows in bf16 with 8 alternatives 124 (4.8 TB/s; a copy 5.1); 64 rows in 32 bits with 20 alternatives
+// 19.7, 8 rows in bf16 with 5 11.9: a launch that joins (5) and finding the alternatives (64 rows without any 10), which is vector work
+// of every wavefront, sorting networks of 64 keys.  So what a wavefront has in its registers, four spans, goes into the first bound at once: by
+// the first span only, 132, 21.8 and 13.2.
 #ifndef LI_LOGPROBS_HPP
 #define LI_LOGPROBS_HPP
 
@@ -19,7 +20,7 @@
 
 namespace {
 
-constexpr uint32_t kLogThreads = 256, kLogWaves = kLogThreads / kLanes, kJoinWaves = 16, kMostTop = 64;
+constexpr uint32_t kLogThreads = 256, kLogWaves = kLogThreads / kLanes, kMostTop = 64;
 constexpr uint32_t kSpan = 8 * kLanes;              // entries that a wavefront looks at at once
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f, kRise = 8.0f;
 
@@ -123,16 +124,22 @@ __device__ __forceinline__ Sums joined(Sums a, Sums b, float c) {
     return Sums{m, a.s + b.s, a.q + b.q, 0.0f};
 }
 
+// The token that was given and its logit, two loads one after the other: asked for before there is anything to do with them.
+struct Given {
+    float logit;
+    bool there;
+};
+template <typename E> __device__ __forceinline__ Given given(const LogParams& p, uint32_t row) {
+    const int32_t token = p.tokens ? p.tokens[row] : -1;
+    const bool there = token >= 0 && (uint32_t)token < p.vocab;
+    return Given{there ? (float)reinterpret_cast<const E*>(p.logits + (int64_t)row * p.stride)[token] : 0.0f, there};
+}
+
 // What a row's sums and largest logits say.
-template <typename E> __device__ __forceinline__ void answer(const LogParams& p, uint32_t row, Sums x, uint64_t key, uint32_t lane) {
+template <typename E> __device__ __forceinline__ void answer(const LogParams& p, uint32_t row, Given t, Sums x, uint64_t key, uint32_t lane) {
     const float log = log2f(x.s);
     auto log_p = [&](float logit) { return ((logit - x.m) * p.c - log) * kLn2; };
-    if (lane == 0 && p.logprob) {
-        const int32_t token = p.tokens[row];
-        float r = 0.0f;
-        if (token >= 0 && (uint32_t)token < p.vocab) r = x.s == 0.0f ? -INFINITY : log_p((float)reinterpret_cast<const E*>(p.logits + (int64_t)row * p.stride)[token]);
-        p.logprob[row] = r;
-    }
+    if (lane == 0 && p.logprob) p.logprob[row] = !t.there ? 0.0f : x.s == 0.0f ? -INFINITY : log_p(t.logit);
     if (lane == 0 && p.entropy) p.entropy[row] = x.s == 0.0f ? 0.0f : (log - x.q / x.s) * kLn2;
     if (lane < p.top) {
         p.top_id[(uint64_t)row * p.top + lane] = key ? (int32_t)token_of(key) : -1;
@@ -159,7 +166,7 @@ template <uint32_t W> __device__ __forceinline__ void gather(Sums* x, uint64_t* 
 }
 
 template <typename E> __global__ __launch_bounds__(kLogThreads) void k_logprobs(const LogParams p) {
-    constexpr uint32_t kAtOnce = sizeof(E) == 4 ? 2 : 4;               // spans that a wavefront has on their way
+    constexpr uint32_t kAtOnce = 4;                                    // spans that a wavefront has on their way
     constexpr uint32_t kStride = kLogWaves * kSpan * kAtOnce;
     __shared__ uint64_t lds_new[kLogWaves][2 * kLanes];
     const uint32_t lane = threadIdx.x % kLanes, wave = uniform(threadIdx.x / kLanes);
@@ -170,6 +177,8 @@ template <typename E> __global__ __launch_bounds__(kLogThreads) void k_logprobs(
     const int64_t begin = (int64_t)odd + (int64_t)z * p.piece, end = min(begin + p.piece, (int64_t)odd + p.vocab);
     const float c = p.c;
 
+    Given token{};
+    if (p.pieces == 1 && wave == 0) token = given<E>(p, row);
     Sums x{-INFINITY, 0.0f, 0.0f, 0.0f};
     float limit = -INFINITY, ref = 0.0f;                               // the last logit that m does for; m, or 0 while there is none
     float s = 0.0f, q = 0.0f;
@@ -189,11 +198,7 @@ template <typename E> __global__ __launch_bounds__(kLogThreads) void k_logprobs(
         x.m = to, s = r.s, q = r.q;
         ref = to > -INFINITY ? to : 0.0f, limit = to + kRise / c;
     };
-    auto take = [&](const Piece8<E>& e, int64_t first) {
-        float largest = e[0];
-#pragma unroll
-        for (uint32_t i = 1; i < 8; ++i) largest = fmaxf(largest, e[i]);
-        if (__any(largest > limit)) raise(largest);
+    auto add = [&](const Piece8<E>& e) {
         float s8 = 0.0f, q8 = 0.0f;
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i) {
@@ -201,28 +206,22 @@ template <typename E> __global__ __launch_bounds__(kLogThreads) void k_logprobs(
             s8 += w, q8 = fmaf(w, fmaxf(d, -1000.0f), q8);             // minus infinity would make 0 times it no number
         }
         s += s8, q += q8;
-        if (p.top && __any(largest > least)) {
-            if (!begun) {
-                // Of the lanes' largest entries the one in the last place that is asked for: below it lies no alternative.
-                const uint32_t last = (uint32_t)__builtin_amdgcn_readlane(rising(order_of(largest), lane), kLanes - p.top);
-                if (from_order(last) > -INFINITY) least = from_order(last - (last == 0x80000000u ? 2 : 1));   // zero is two numbers
-                begun = true;
-            }
-            const float before = least;                                // of equal ones a lower token may still come in this span, not in later ones
+    };
+    auto collect = [&](const Piece8<E>& e, int64_t first) {
+        const float before = least;                                    // of equal ones a lower token may still come in this span, not in later ones
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
-                const bool above = e[i] > before;
-                const uint64_t who = __ballot(above);
-                if (!who) continue;
-                if (above) buf[waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] =
-                    key_of(e[i], (uint32_t)(first + Piece8<E>::place(lane, i) - odd));
-                waiting += (uint32_t)__popcll(who);
-                if (waiting >= kLanes) {
-                    merge(kLanes);
-                    waiting -= kLanes;
-                    const uint64_t rest = lane < waiting ? buf[kLanes + lane] : 0;
-                    buf[lane] = rest;
-                }
+        for (uint32_t i = 0; i < 8; ++i) {
+            const bool above = e[i] > before;
+            const uint64_t who = __ballot(above);
+            if (!who) continue;
+            if (above) buf[waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] =
+                key_of(e[i], (uint32_t)(first + Piece8<E>::place(lane, i) - odd));
+            waiting += (uint32_t)__popcll(who);
+            if (waiting >= kLanes) {
+                merge(kLanes);
+                waiting -= kLanes;
+                const uint64_t rest = lane < waiting ? buf[kLanes + lane] : 0;
+                buf[lane] = rest;
             }
         }
     };
@@ -234,16 +233,36 @@ template <typename E> __global__ __launch_bounds__(kLogThreads) void k_logprobs(
             if (from >= begin && from + kSpan <= end) e[u] = load8<E>(base, from, lane);
             else e[u] = load8_within<E>(base, from, lane, begin, end);
         }
+        float most[kAtOnce], largest = -INFINITY;
+#pragma unroll
+        for (uint32_t u = 0; u < kAtOnce; ++u) {
+            most[u] = e[u][0];
+#pragma unroll
+            for (uint32_t i = 1; i < 8; ++i) most[u] = fmaxf(most[u], e[u][i]);
+            largest = fmaxf(largest, most[u]);
+        }
+        if (__any(largest > limit)) raise(largest);
 #pragma unroll
         for (uint32_t u = 0; u < kAtOnce; ++u)
-            if (first + u * kSpan < end) take(e[u], first + u * kSpan);
+            if (first + u * kSpan < end) add(e[u]);
+        if (p.top && __any(largest > least)) {
+            if (!begun) {
+                // Of the lanes' largest entries the one in the last place that is asked for: below it lies no alternative.
+                const uint32_t last = (uint32_t)__builtin_amdgcn_readlane(rising(order_of(largest), lane), kLanes - p.top);
+                if (from_order(last) > -INFINITY) least = from_order(last - (last == 0x80000000u ? 2 : 1));   // zero is two numbers
+                begun = true;
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < kAtOnce; ++u)
+                if (__any(most[u] > least)) collect(e[u], first + u * kSpan);
+        }
     }
     if (p.top && waiting) merge(waiting);
     x.s = wave_sum(s), x.q = wave_sum(q);
     gather<kLogWaves>(&x, &key, wave, lane, p.top != 0, p.c);
     if (wave != 0) return;
     if (p.pieces == 1) {
-        answer<E>(p, row, x, key, lane);
+        answer<E>(p, row, token, x, key, lane);
     } else {
         if (lane == 0) p.part_sums[blockIdx.x] = x;
         if (lane < p.top) p.part_keys[(uint64_t)blockIdx.x * p.top + lane] = key;
@@ -251,19 +270,21 @@ template <typename E> __global__ __launch_bounds__(kLogThreads) void k_logprobs(
 }
 
 // The pieces of a row.
-template <typename E> __global__ __launch_bounds__(kJoinWaves * kLanes) void k_join_logprobs(const LogParams p) {
+template <typename E, uint32_t W> __global__ __launch_bounds__(W * kLanes) void k_join_logprobs(const LogParams p) {
     const uint32_t lane = threadIdx.x % kLanes, wave = uniform(threadIdx.x / kLanes), row = blockIdx.x;
+    Given token{};
+    if (wave == 0) token = given<E>(p, row);
     Sums x{-INFINITY, 0.0f, 0.0f, 0.0f};
     uint64_t key = 0;
-    for (uint32_t z = wave; z < p.pieces; z += kJoinWaves) {
+    for (uint32_t z = wave; z < p.pieces; z += W) {
         const uint64_t at = (uint64_t)row * p.pieces + z;
         const uint32_t from = kLanes - 1 - lane;                       // in rising order
         const uint64_t theirs = from < p.top ? p.part_keys[at * p.top + from] : 0;
         x = joined(x, p.part_sums[at], p.c);
         if (p.top) key = settled(max(key, theirs), lane);
     }
-    gather<kJoinWaves>(&x, &key, wave, lane, p.top != 0, p.c);
-    if (wave == 0) answer<E>(p, row, x, key, lane);
+    gather<W>(&x, &key, wave, lane, p.top != 0, p.c);
+    if (wave == 0) answer<E>(p, row, token, x, key, lane);
 }
 
 }  // namespace
