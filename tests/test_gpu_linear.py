@@ -229,3 +229,30 @@ def test_more_outputs_than_one_tile_has_with_many_rows(tokens):
     gate, up = (Matrix(600, 384, 128, "bf16", seed=95 + i) for i in range(2))
     x = rows(tokens, 384, "bf16", seed=97)
     check_gated(gate, up, x, gated(gate, up, x), "silu")
+
+
+@pytest.mark.parametrize("tokens", [8, 32, 40, 64, 65, 200])
+@pytest.mark.parametrize("group", [32, 64])
+def test_what_is_not_a_number_stays_in_its_row_with_small_groups(tokens, group):
+    m = Matrix(72, 328, group, "fp16", seed=100)
+    x = rows(tokens, 328, "fp16", seed=101).contiguous()
+    clean = m.linear(x).clone()
+    x[tokens // 3, 70], x[tokens - 1, 300] = float("nan"), float("-inf")
+    y = m.linear(x)
+    odd = torch.zeros(tokens, dtype=torch.bool, device="cuda")
+    odd[[tokens // 3, tokens - 1]] = True
+    assert torch.equal(y[~odd], clean[~odd])
+    assert torch.isnan(y[tokens // 3]).all() and not torch.isfinite(y[tokens - 1]).any()
+
+
+@pytest.mark.parametrize("tokens", [1, 8, 16, 32, 64, 200])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_a_weight_that_is_not_a_number_reaches_its_output_only(tokens, group):
+    m = Matrix(40, 264, group, "bf16", seed=102)
+    x = rows(tokens, 264, "bf16", seed=103)
+    clean = m.linear(x).clone()
+    m.pairs[7, 0, 1], m.pairs[33, 264 // group, 0] = float("nan"), float("nan")
+    y = m.linear(x)
+    odd = torch.zeros(40, dtype=torch.bool, device="cuda")
+    odd[[7, 33]] = True
+    assert torch.equal(y[:, ~odd], clean[:, ~odd]) and torch.isnan(y[:, odd]).all()
