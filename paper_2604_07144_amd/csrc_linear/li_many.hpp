@@ -159,8 +159,9 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
             }
         }
     }
-    // Results go through LDS, a tile of tokens at a time, so that neighbouring threads have neighbouring outputs.
+    // Results go through LDS, a tile of tokens at a time, so that a thread has four neighbouring outputs, and neighbouring threads the next.
     constexpr uint32_t kWide = kManyWaves * kOuts * 16, kRow = kWide * (kGated ? 2 : 1) + 4;
+    const bool at_once = four_at_once(p);
     float* const out = reinterpret_cast<float*>(lds);                                       // [16 tokens][output, of both matrices]
 #pragma unroll
     for (uint32_t i = 0; i < TT; ++i) {
@@ -171,10 +172,11 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
             for (uint32_t j = 0; j < 4; ++j) out[(q * 4 + j) * kRow + (kGated && r >= kOuts ? kWide : 0) + wave * kOuts * 16 + r % kOuts * 16 + col] = acc[r][i][j];
         __syncthreads();
 #pragma unroll 1
-        for (uint32_t e = threadIdx.x; e < 16 * kWide; e += kManyWaves * kLanes) {
+        for (uint32_t e = threadIdx.x * 4; e < 16 * kWide; e += kManyWaves * kLanes * 4) {
             const uint32_t t = t0 + i * 16 + e / kWide, n = n0 - wave * kOuts * 16 + e % kWide;
             const float* from = out + e / kWide * kRow + e % kWide;
-            if (t < p.n_tokens && n < p.w[0].n_out) put<E, kGated>(p, part, n, t, from[0], kGated ? from[kWide] : 0.0f);
+            const f32x4 a = *reinterpret_cast<const f32x4*>(from), b = *reinterpret_cast<const f32x4*>(from + (kGated ? kWide : 0));
+            if (t < p.n_tokens && n < p.w[0].n_out) put4<E, kGated>(p, at_once, part, n, t, a, b);
         }
     }
 }
