@@ -64,7 +64,7 @@ constexpr uint32_t kMostFew = 64;
 
 // Estimates of the kernel of many rows, us: what a workgroup's step of 128 columns takes besides its tiles of 16 tokens and for each
 // of them, what comes before the first and after the last step, what a second launch costs, and bytes of parts that are written and read a us.
-constexpr double kStepUs = 0.3, kTileUs = 0.46, kEnterUs = 8, kJoinUs = 4, kPartBytesPerUs = 4e6;
+constexpr double kStepUs = 0.3, kTileUs = 0.46, kEnterUs = 5, kJoinUs = 4, kPartBytesPerUs = 4e6;
 
 ap_status linear_plan(const Weights& w, uint32_t n_tokens, uint32_t group, bool gated, LinearPlan* out) {
     LinearPlan r{};
@@ -141,7 +141,7 @@ ap_status run_linear(LinearParams p, const LinearPlan& plan, uint32_t dtype, uin
         });
         if (plan.n_parts > 1) {
             auto join = gated ? k_join_parts<decltype(e), true> : k_join_parts<decltype(e), false>;
-            hipLaunchKernelGGL(join, dim3(tiles_of((uint64_t)p.n_tokens * p.w[0].n_out, 256)), dim3(256), 0, on, p);
+            hipLaunchKernelGGL(join, dim3(tiles_of((uint64_t)p.n_tokens * tiles_of(p.w[0].n_out, 4), 256)), dim3(256), 0, on, p);
         }
     });
     return launched();

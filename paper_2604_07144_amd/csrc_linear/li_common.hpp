@@ -125,25 +125,20 @@ template <typename E, bool kGated> __device__ __forceinline__ void put(const Lin
     if (kGated) row[p.w[0].n_out] = b;
 }
 
-// Whether four neighbouring outputs, from a multiple of four on, can be written at once.
-__device__ __forceinline__ bool four_at_once(const LinearParams& p) {
-    if (p.n_parts > 1) return p.w[0].n_out % 4 == 0;
+// Whether four neighbouring outputs, from a multiple of four on, can be written at once: results; sums of parts.
+__device__ __forceinline__ bool four_results(const LinearParams& p) {
     uintptr_t all = reinterpret_cast<uintptr_t>(p.y) | (uintptr_t)p.y_stride;
     if (p.add) all |= reinterpret_cast<uintptr_t>(p.add) | (uintptr_t)p.add_stride;
     return all % 8 == 0;
 }
-// put of the four outputs from n on, a multiple of four; those that there are.
-template <typename E, bool kGated> __device__ __forceinline__ void put4(const LinearParams& p, bool at_once, uint32_t part, uint32_t n, uint32_t t, f32x4 a, f32x4 b) {
+__device__ __forceinline__ bool four_sums(const LinearParams& p) { return p.w[0].n_out % 4 == 0; }
+
+// finish and put of the four outputs from n on, a multiple of four; those that there are.
+template <typename E, bool kGated> __device__ __forceinline__ void finish4(const LinearParams& p, bool at_once, uint32_t t, uint32_t n, f32x4 a, f32x4 b) {
     if (!at_once || n + 4 > p.w[0].n_out) {
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j)
-            if (n + j < p.w[0].n_out) put<E, kGated>(p, part, n + j, t, a[j], b[j]);
-        return;
-    }
-    if (p.n_parts > 1) {
-        float* row = p.parts + ((uint64_t)part * p.n_tokens + t) * ((kGated ? 2 : 1) * (uint64_t)p.w[0].n_out) + n;
-        *reinterpret_cast<f32x4*>(row) = a;
-        if (kGated) *reinterpret_cast<f32x4*>(row + p.w[0].n_out) = b;
+            if (n + j < p.w[0].n_out) finish<E, kGated>(p, t, n + j, a[j], b[j]);
         return;
     }
     if constexpr (kGated) {
@@ -154,6 +149,18 @@ template <typename E, bool kGated> __device__ __forceinline__ void put4(const Li
         a += f32x4{low16<E>(x[0]), high16<E>(x[0]), low16<E>(x[1]), high16<E>(x[1])};
     }
     *reinterpret_cast<u32x2*>(p.y + (int64_t)t * p.y_stride + 2ull * n) = u32x2{pack2<E>(a[0], a[1]), pack2<E>(a[2], a[3])};
+}
+template <typename E, bool kGated> __device__ __forceinline__ void put4(const LinearParams& p, bool at_once, uint32_t part, uint32_t n, uint32_t t, f32x4 a, f32x4 b) {
+    if (p.n_parts == 1) return finish4<E, kGated>(p, at_once, t, n, a, b);
+    if (!at_once) {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+            if (n + j < p.w[0].n_out) put<E, kGated>(p, part, n + j, t, a[j], b[j]);
+        return;
+    }
+    float* row = p.parts + ((uint64_t)part * p.n_tokens + t) * ((kGated ? 2 : 1) * (uint64_t)p.w[0].n_out) + n;
+    *reinterpret_cast<f32x4*>(row) = a;
+    if (kGated) *reinterpret_cast<f32x4*>(row + p.w[0].n_out) = b;
 }
 
 }  // namespace

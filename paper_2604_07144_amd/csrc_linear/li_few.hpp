@@ -282,19 +282,27 @@ __global__ __launch_bounds__((FewShape<G, T, kGated, kHeld>::kWaves * kLanes)) v
     }
 }
 
-// Sums of the parts, in order.
+// Sums of the parts, in order; four outputs a thread.  (Parts are asked for only where all sums of one are fewer than 2^32.)
 template <typename E, bool kGated> __global__ __launch_bounds__(256) void k_join_parts(const LinearParams p) {
-    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint32_t t = (uint32_t)(at / p.w[0].n_out), n = (uint32_t)(at % p.w[0].n_out);
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, n_out = p.w[0].n_out, fours = (n_out + 3) / 4, t = at / fours, n = at % fours * 4;
     if (t >= p.n_tokens) return;
-    const uint64_t width = (kGated ? 2 : 1) * (uint64_t)p.w[0].n_out;
+    const uint64_t width = (kGated ? 2 : 1) * (uint64_t)n_out;
     const float* from = p.parts + (uint64_t)t * width + n;
-    float a = 0.0f, b = 0.0f;
+    const bool at_once = four_sums(p);
+    auto four = [&](const float* x) {
+        if (at_once) return *reinterpret_cast<const f32x4*>(x);
+        f32x4 r = {};
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+            if (n + j < n_out) r[j] = x[j];
+        return r;
+    };
+    f32x4 a = {}, b = {};
     for (uint32_t z = 0; z < p.n_parts; ++z, from += (uint64_t)p.n_tokens * width) {
-        a += from[0];
-        if (kGated) b += from[p.w[0].n_out];
+        a += four(from);
+        if (kGated) b += four(from + n_out);
     }
-    finish<E, kGated>(p, t, n, a, b);
+    finish4<E, kGated>(p, four_results(p), t, n, a, b);
 }
 
 }  // namespace

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kManyWaves * kLanes) void k_linear_many(const Linea
     }
     // Results go through LDS, a tile of tokens at a time, so that a thread has four neighbouring outputs, and neighbouring threads the next.
     constexpr uint32_t kWide = kManyWaves * kOuts * 16, kRow = kWide * (kGated ? 2 : 1) + 4;
-    const bool at_once = four_at_once(p);
+    const bool at_once = p.n_parts == 1 ? four_results(p) : four_sums(p);
     float* const out = reinterpret_cast<float*>(lds);                                       // [16 tokens][output, of both matrices]
 #pragma unroll
     for (uint32_t i = 0; i < TT; ++i) {

@@ -256,3 +256,18 @@ def test_a_weight_that_is_not_a_number_reaches_its_output_only(tokens, group):
     odd = torch.zeros(40, dtype=torch.bool, device="cuda")
     odd[[7, 33]] = True
     assert torch.equal(y[:, ~odd], clean[:, ~odd]) and torch.isnan(y[:, odd]).all()
+
+
+@pytest.mark.parametrize("tokens", [9, 33, 70, 130])
+@pytest.mark.parametrize("n_out,apart,skip", [(516, 0, 0), (516, 1, 0), (516, 4, 1), (516, 4, 2), (516, 4, 4), (514, 2, 4), (513, 0, 3)])
+def test_results_at_places_of_any_kind(tokens, n_out, apart, skip):
+    """Rows of y and of what is added that begin anywhere and are any distance apart; what lies between them stays."""
+    m = Matrix(n_out, 1536, 64, "bf16", seed=110)
+    x = rows(tokens, 1536, "bf16", seed=111)
+    far = n_out + skip + apart
+    space = torch.full((tokens, far), 3.0, dtype=torch.bfloat16, device="cuda")
+    before = rows(tokens, far, "bf16", seed=112).contiguous()
+    y, add = space[:, skip:skip + n_out], before[:, skip:skip + n_out]
+    m.linear(x, add, y)
+    check_linear(m, x, y, add)
+    assert (space[:, :skip] == 3.0).all() and (space[:, skip + n_out:] == 3.0).all()
