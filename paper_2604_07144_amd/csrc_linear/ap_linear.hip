@@ -58,13 +58,14 @@ struct LinearPlan {
 constexpr uint32_t kCus = 256;
 
 // Up to kMostFew tokens go to the kernel of few rows, whose workgroup has all of them and 128 outputs or fewer; the other one's has
-// 512 outputs.  64 tokens, few / many, bf16, groups of 128, us: 4096 outputs of 4096 inputs 14.6 / 24.6, 4096 of 14336 26 / 37, 10240 of 8192
-// 32 / 42, gated 14336 of 4096 38 / 43.
+// 512 outputs.  64 tokens, few / many, bf16, groups of 128, us: 4096 outputs of 4096 inputs 15.2 / 19.7, 4096 of 14336 25 / 31, 10240 of
+// 8192 31 / 34, gated 14336 of 4096 36 / 40.
 constexpr uint32_t kMostFew = 64;
 
 // Estimates of the kernel of many rows, us: what a workgroup's step of 128 columns takes besides its tiles of 16 tokens and for each
 // of them, what comes before the first and after the last step, what a second launch costs, and bytes of parts that are written and read a us.
-constexpr double kStepUs = 0.3, kTileUs = 0.46, kEnterUs = 5, kJoinUs = 4, kPartBytesPerUs = 4e6;
+// (With 5 for 8, what a single tile takes now, 2048 tokens of 14336 gated outputs of 4096 get tiles of 64 for 96: 579 us for 539.)
+constexpr double kStepUs = 0.3, kTileUs = 0.46, kEnterUs = 8, kJoinUs = 4, kPartBytesPerUs = 4e6;
 
 ap_status linear_plan(const Weights& w, uint32_t n_tokens, uint32_t group, bool gated, LinearPlan* out) {
     LinearPlan r{};
