@@ -112,6 +112,14 @@ __device__ __forceinline__ uint64_t of_lane(uint64_t key, uint32_t lane) {
     return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(key >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)key, lane);
 }
 
+// Between what lanes of a wavefront write to LDS and what others read of it, or write in its place.  The LDS has a wavefront's operations in
+// order; this keeps the compiler, for which lanes are threads of their own, from moving or merging them.  It costs no instruction.
+__device__ __forceinline__ void in_order() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // What sums that were taken against x.m are worth against `to`, which is not below it.
 __device__ __forceinline__ Sums moved(Sums x, float to, float c) {
     if (x.m == to || x.m == -INFINITY) return Sums{to, x.s, x.q, 0.0f};
@@ -188,6 +196,7 @@ template <typename E> __global__ __launch_bounds__(kLogThreads) void k_logprobs(
     bool begun = false;
     uint64_t* const buf = lds_new[wave];
     auto merge = [&](uint32_t n) {
+        in_order();
         key = settled(max(key, rising(lane < n ? buf[lane] : 0, lane)), lane);
         const uint64_t last = of_lane(key, p.top - 1);
         if (last) least = value_of(last);
@@ -222,6 +231,7 @@ template <typename E> __global__ __launch_bounds__(kLogThreads) void k_logprobs(
                 waiting -= kLanes;
                 const uint64_t rest = lane < waiting ? buf[kLanes + lane] : 0;
                 buf[lane] = rest;
+                in_order();
             }
         }
     };

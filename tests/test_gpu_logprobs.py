@@ -209,3 +209,17 @@ def test_far_rows():
     x = wide[:, 7:1507]
     x.copy_(_logits(3, 1500, "fp32", 12))
     _check(_run(x, [3, 4, 5], 1.0, 5, "fp32"), x, [3, 4, 5], 1.0, 5)
+
+
+@pytest.mark.parametrize("dtype,width", [("bf16", 8), ("fp32", 4)])
+@pytest.mark.parametrize("lane", [0, 37, 63])
+def test_alternatives_that_one_lane_finds(dtype, width, lane):
+    """Neighbouring tokens of a span that go up from span to span: one lane writes what the others merge, and new ones follow in the same places."""
+    vocab, span = 512 * 40, 512 if dtype == "bf16" else 256
+    for n in (2, 600):
+        x = torch.full((n, vocab), -9.0, device="cuda")
+        at = (torch.arange(vocab // span, device="cuda") * span + lane * width)[:, None] + torch.arange(width, device="cuda")
+        x[:, at.flatten()] = torch.arange(at.numel(), device="cuda").float() * 2.0 ** -5
+        x = x.to(TYPES[dtype][0]).contiguous()
+        tokens = np.full(n, vocab - 1)
+        _check(_run(x, tokens, 1.0, 64, dtype), x, tokens, 1.0, 64, (0, n - 1))
