@@ -85,7 +85,8 @@ typedef struct {
     int64_t stride;
 } ap_logits;
 
-/* With p = e^s / sum e^s over s = scale * logits (scale > 0, one over the temperature; log2(e) times it is finite), of each row:
+/* With p = e^s / sum e^s over s = scale * logits (one over the temperature; log2(e) times it is at least 2^-120 and finite), of each
+ * row:
  *   logprob     : log p of tokens[row], 0 where that is outside [0, vocab); tokens may be NULL, then logprob is too.
  *   entropy     : - sum p log p; may be NULL.
  *   top_id, top_logprob : [n_rows][top], the `top` (at most 64) tokens of the largest logits, of equal ones the lowest token

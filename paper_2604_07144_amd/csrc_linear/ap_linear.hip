@@ -275,7 +275,7 @@ ap_status ap_logprobs(const ap_logits* logits, const int32_t* tokens, float scal
     LogPlan plan;
     const ap_status st = take_logits(logits, top, &plan);
     if (st != AP_OK) return st;
-    if (!(scale * kLog2e > 0.0f) || !std::isfinite(scale * kLog2e) || (tokens == nullptr) != (logprob == nullptr) || (top && (!top_id || !top_logprob))) return AP_ERR_INVALID;
+    if (!(scale * kLog2e >= kLeastScale) || !std::isfinite(scale * kLog2e) || (tokens == nullptr) != (logprob == nullptr) || (top && (!top_id || !top_logprob))) return AP_ERR_INVALID;
     if (!multiple(tokens, 4) || !multiple(logprob, 4) || !multiple(entropy, 4) || (top && (!multiple(top_id, 4) || !multiple(top_logprob, 4)))) return AP_ERR_INVALID;
     if (!space_ok(workspace, workspace_bytes, plan.bytes)) return AP_ERR_INVALID;
     if (logits->n_rows == 0) return AP_OK;

@@ -23,6 +23,9 @@ namespace {
 constexpr uint32_t kLogThreads = 256, kLogWaves = kLogThreads / kLanes, kMostTop = 64;
 constexpr uint32_t kSpan = 8 * kLanes;              // entries that a wavefront looks at at once
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f, kRise = 8.0f;
+// The least c.  A logit may then be above m by 8 / c = 2^123 without passing it by more than kRise, and where (x - m) passes 32 bits below it
+// d is under -2^8 and 2^d is no part of a sum in 32 bits.  With smaller ones differences that count would be infinite.
+constexpr float kLeastScale = 0x1p-120f;
 
 struct Sums {
     float m, s, q, unused;                          // m is minus infinity where nothing was seen

@@ -180,3 +180,10 @@ def test_every_code_has_a_place_of_its_own():
     words = np.zeros((1, 16), np.uint32)
     words[0, orc.place(77)[0]] = np.uint32(11) << np.uint32(orc.place(77)[1])
     assert np.nonzero(orc.values(words, np.array([[[1.0, 0.0]]]), 128, 128)[0])[0].tolist() == [77]
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -121, 1e-38, 1e-45])
+def test_scales_that_are_too_small(scale):
+    """Below 2^-120 (times log2(e)) logits in 32 bits could be further apart than 32 bits hold, and yet both count."""
+    _refused(b.AP_ERR_INVALID, b.ap_logprobs, _logits(dtype=b.AP_FP32, stride=4000), AT, scale, 5, AT, AT, AT, AT, AT, 1 << 40)
+    b.ap_logprobs(_logits(n_rows=0), AT, 2.0 ** -120, 5, AT, AT, AT, AT)
