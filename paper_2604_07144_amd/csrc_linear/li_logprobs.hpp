@@ -148,6 +148,7 @@ template <typename E> __device__ __forceinline__ Given given(const LogParams& p,
 
 // What a row's sums and largest logits say.
 template <typename E> __device__ __forceinline__ void answer(const LogParams& p, uint32_t row, Given t, Sums x, uint64_t key, uint32_t lane) {
+    if (!(x.s < INFINITY)) x.s = __builtin_nanf("");                   // an infinity that no limit in 32 bits lay below was a weight, and not no number
     const float log = log2f(x.s);
     auto log_p = [&](float logit) { return ((logit - x.m) * p.c - log) * kLn2; };
     if (lane == 0 && p.logprob) p.logprob[row] = !t.there ? 0.0f : x.s == 0.0f ? -INFINITY : log_p(t.logit);

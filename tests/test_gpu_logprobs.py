@@ -223,3 +223,14 @@ def test_alternatives_that_one_lane_finds(dtype, width, lane):
         x = x.to(TYPES[dtype][0]).contiguous()
         tokens = np.full(n, vocab - 1)
         _check(_run(x, tokens, 1.0, 64, dtype), x, tokens, 1.0, 64, (0, n - 1))
+
+
+
+@pytest.mark.parametrize("rows", [2, 700])
+def test_an_infinity_among_the_largest_numbers(rows):
+    """Nothing in 32 bits lies above the largest logits by as much as would raise the reference."""
+    x = torch.full((rows, 33000), torch.finfo(torch.float32).max, device="cuda")
+    x[1, 32000] = float("inf")
+    got = _run(x, [5] * rows, 2.0 ** -120, 2, "fp32")
+    assert np.isnan(got["logprob"][1]) and np.isnan(got["entropy"][1]) and np.isnan(got["tops"][1]).all()
+    assert np.abs(got["logprob"][0] + np.log(33000)) <= 1e-5
