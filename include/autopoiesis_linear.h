@@ -93,7 +93,7 @@ typedef struct {
  *                 first, and their log p.  Places beyond the tokens that are above minus infinity get -1 and minus infinity.
  * A logit of minus infinity is a token that is ruled out.  In a row where all are, log p is minus infinity and the entropy 0.  Where
  * a row holds a NaN or plus infinity, its logprob, entropy and top_logprob are NaN (0 still where no token is given), and what is
- * not a number is no alternative.  Sums are in 32 bits. */
+ * not a number is no alternative.  Sums are in 32 bits; what is made of them is in 64, and rounded once. */
 ap_status ap_logprobs_workspace(const ap_logits *logits, uint32_t top, uint64_t *bytes);
 ap_status ap_logprobs(const ap_logits *logits, const int32_t *tokens, float scale, uint32_t top, float *logprob, float *entropy,
                       int32_t *top_id, float *top_logprob, void *workspace, uint64_t workspace_bytes, void *stream);

@@ -282,7 +282,8 @@ ap_status ap_logprobs(const ap_logits* logits, const int32_t* tokens, float scal
     LogParams p{};
     p.logits = (const char*)logits->data, p.stride = logits->stride, p.n_rows = logits->n_rows, p.vocab = logits->vocab;
     p.top = top, p.pieces = plan.pieces, p.piece = plan.piece;
-    p.tokens = tokens, p.c = scale * kLog2e, p.logprob = logprob, p.entropy = entropy, p.top_logprob = top_logprob, p.top_id = top_id;
+    p.c = scale * kLog2e, p.scale = scale, p.beyond_c = p.scale / (p.c * kLn2) - 1.0;
+    p.tokens = tokens, p.logprob = logprob, p.entropy = entropy, p.top_logprob = top_logprob, p.top_id = top_id;
     p.part_sums = (Sums*)workspace, p.part_keys = (uint64_t*)((char*)workspace + (uint64_t)p.n_rows * p.pieces * 16);
     for_logits(logits->dtype, [&](auto e) {
         using E = decltype(e);

@@ -22,7 +22,8 @@ namespace {
 
 constexpr uint32_t kLogThreads = 256, kLogWaves = kLogThreads / kLanes, kMostTop = 64;
 constexpr uint32_t kSpan = 8 * kLanes;              // entries that a wavefront looks at at once
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f, kRise = 8.0f;
+constexpr float kLog2e = 1.44269504088896341f, kRise = 8.0f;
+constexpr double kLn2 = 0.693147180559945309;
 // The least c.  A logit may then be above m by 8 / c = 2^123 without passing it by more than kRise, and where (x - m) passes 32 bits below it
 // d is under -2^8 and 2^d is no part of a sum in 32 bits.  With smaller ones differences that count would be infinite.
 constexpr float kLeastScale = 0x1p-120f;
@@ -36,7 +37,8 @@ struct LogParams {
     int64_t stride;
     uint32_t n_rows, vocab, top, pieces, piece;     // a row is cut into pieces of `piece` entries
     const int32_t* tokens;
-    float c;
+    float c;                                        // log2(e) scale, rounded
+    double scale, beyond_c;                         // the scale as it was given; log2(e) scale / c - 1
     float *logprob, *entropy, *top_logprob;
     int32_t* top_id;
     Sums* part_sums;                                // [row][piece]
@@ -146,13 +148,34 @@ template <typename E> __device__ __forceinline__ Given given(const LogParams& p,
     return Given{there ? (float)reinterpret_cast<const E*>(p.logits + (int64_t)row * p.stride)[token] : 0.0f, there};
 }
 
-// What a row's sums and largest logits say.
+// log s to 64 bits, of a number above 0: with s = 2^k f, f from sqrt(1/2) to sqrt(2), it is k log 2 + 2 atanh z, z = (f - 1) / (f + 1), whose series
+// (z^2 is at most 0.03) is left after z^21.  As short as it can be, since a row's last steps wait for it.
+__device__ __forceinline__ double log_of(float s) {
+    float f = __builtin_amdgcn_frexp_mantf(s);
+    const bool low = f < 0.70710678f;
+    f = low ? 2.0f * f : f;
+    const double k = __builtin_amdgcn_frexp_expf(s) - (low ? 1 : 0), d = (double)f + 1.0;
+    double inverse = __builtin_amdgcn_rcp(d);                          // to 2^-20 or so, then 2^-40 and 2^-52
+    inverse = fma(fma(-d, inverse, 1.0), inverse, inverse);
+    inverse = fma(fma(-d, inverse, 1.0), inverse, inverse);
+    const double z = ((double)f - 1.0) * inverse, w = z * z, v = w * w;
+    double even = 1.0 / 21, odd = 1.0 / 19;                            // from z^5 and z^3 on, in steps of z^4
+    even = fma(even, v, 1.0 / 17), odd = fma(odd, v, 1.0 / 15);
+    even = fma(even, v, 1.0 / 13), odd = fma(odd, v, 1.0 / 11);
+    even = fma(even, v, 1.0 / 9), odd = fma(odd, v, 1.0 / 7);
+    even = fma(even, v, 1.0 / 5), odd = fma(odd, v, 1.0 / 3);
+    return fma(k, kLn2, 2.0 * fma(z * w, fma(even, w, odd), z));
+}
+
+// What a row's sums and largest logits say.  Once a row and so in 64 bits, with the scale itself: differences of logits that pass 32 bits are
+// numbers here, and beside what the sums are off there is one rounding (8 rows of 128256: 12.35 us for 12.1 in 32 bits).  The sums were taken with c, which is rounded; what that makes of
+// log S goes by the mean of d, to first order, and is put back.
 template <typename E> __device__ __forceinline__ void answer(const LogParams& p, uint32_t row, Given t, Sums x, uint64_t key, uint32_t lane) {
     if (!(x.s < INFINITY)) x.s = __builtin_nanf("");                   // an infinity that no limit in 32 bits lay below was a weight, and not no number
-    const float log = log2f(x.s);
-    auto log_p = [&](float logit) { return ((logit - x.m) * p.c - log) * kLn2; };
+    const double with_c = log_of(x.s), mean = x.q / x.s * kLn2, whole = fma(p.beyond_c, mean, with_c);
+    auto log_p = [&](float logit) { return (float)fma((double)logit - (double)x.m, p.scale, -whole); };
     if (lane == 0 && p.logprob) p.logprob[row] = !t.there ? 0.0f : x.s == 0.0f ? -INFINITY : log_p(t.logit);
-    if (lane == 0 && p.entropy) p.entropy[row] = x.s == 0.0f ? 0.0f : (log - x.q / x.s) * kLn2;
+    if (lane == 0 && p.entropy) p.entropy[row] = x.s == 0.0f ? 0.0f : (float)(with_c - mean);
     if (lane < p.top) {
         p.top_id[(uint64_t)row * p.top + lane] = key ? (int32_t)token_of(key) : -1;
         p.top_logprob[(uint64_t)row * p.top + lane] = x.s != x.s ? x.s : key ? log_p(value_of(key)) : -INFINITY;
@@ -177,7 +200,8 @@ template <uint32_t W> __device__ __forceinline__ void gather(Sums* x, uint64_t* 
     }
 }
 
-template <typename E> __global__ __launch_bounds__(kLogThreads) void k_logprobs(const LogParams p) {
+// Registers for six wavefronts a SIMD (five in 32 bits): the 64 bits of the answer would take one too many.
+template <typename E> __global__ __launch_bounds__(kLogThreads, sizeof(E) == 2 ? 6 : 5) void k_logprobs(const LogParams p) {
     constexpr uint32_t kAtOnce = 4;                                    // spans that a wavefront has on their way
     constexpr uint32_t kStride = kLogWaves * kSpan * kAtOnce;
     __shared__ uint64_t lds_new[kLogWaves][2 * kLanes];

@@ -234,3 +234,45 @@ def test_an_infinity_among_the_largest_numbers(rows):
     got = _run(x, [5] * rows, 2.0 ** -120, 2, "fp32")
     assert np.isnan(got["logprob"][1]) and np.isnan(got["entropy"][1]) and np.isnan(got["tops"][1]).all()
     assert np.abs(got["logprob"][0] + np.log(33000)) <= 1e-5
+
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("scale", [1.0, 0.7, 2.5])
+@pytest.mark.parametrize("vocab", [4097, 65537])
+def test_answers_are_rounded_once(dtype, scale, vocab):
+    """Tokens far below all others, which are alike: the sum is a power of two to 2^-30, so that log p has one rounding of its own, 2^-24."""
+    rng = np.random.default_rng(vocab)
+    n = 200
+    x = torch.zeros((n, vocab), dtype=TYPES[dtype][0], device="cuda")
+    tokens = rng.integers(0, vocab, n)
+    x[torch.arange(n), torch.from_numpy(tokens).cuda()] = torch.from_numpy(-30.0 / scale - 60.0 * rng.random(n)).to(x.dtype).cuda()
+    got = _run(x, tokens, scale, 2, dtype)
+    s = float(np.float32(scale)) * x.double().cpu().numpy()[np.arange(n), tokens]
+    want = s - np.log(vocab - 1.0)
+    assert (np.abs(got["logprob"] - want) <= np.abs(want) * (2.0 ** -24 + 2.0 ** -30)).all()
+
+
+@pytest.mark.parametrize("vocab", [2, 3, 7, 100, 1000, 4099, 30011, 128256])
+@pytest.mark.parametrize("n", [2, 600])
+def test_alike_logits(vocab, n):
+    """The sum is the number of tokens, and everything else one rounding."""
+    x = torch.full((n, vocab), 3.25, dtype=torch.bfloat16, device="cuda")
+    got, want = _run(x, np.arange(n) % vocab, 0.7, 1), np.log(float(vocab))
+    for f, y in (("logprob", -want), ("entropy", want), ("tops", -want)):
+        assert (np.abs(got[f] - y) <= want * (2.0 ** -24 + 2.0 ** -50)).all(), f
+
+
+
+@pytest.mark.parametrize("vocab", [50, 20000])
+def test_logits_whose_difference_passes_32_bits(vocab):
+    """2^-120 is the least that log2(e) times the scale may be: from there on a difference that passes 32 bits is of a token without
+    probability, whose logarithm is a number all the same."""
+    x = torch.full((3, vocab), -3e38, device="cuda")
+    x[:, vocab - 2] = 3e38
+    for scale in (0.25, 1e-30, 2.0 ** -120):
+        got = _run(x, [0, vocab - 2, vocab - 1], scale, 3, "fp32")
+        far = (float(x[0, 0]) - float(x[0, vocab - 2])) * float(np.float32(scale))
+        assert np.abs(got["logprob"] - [far, 0.0, far]).max() <= 2.0 ** -24 * abs(far)
+        assert (got["ids"] == [vocab - 2, 0, 1]).all() and np.abs(got["tops"] - [0.0, far, far]).max() <= 2.0 ** -24 * abs(far)
+        assert (np.abs(got["entropy"]) <= 2.0 ** -100).all()
