@@ -1,9 +1,10 @@
 """Products with weights in 4 bits, and the gated half of a feed-forward block, against plain sums in 64 bits."""
+import numpy as np
 import pytest
 import torch
 
 from paper_2604_07144_amd import binding as b
-from tests.linear_harness import Matrix, check_gated, check_linear, gated, rows, stream_of, vectors
+from tests.linear_harness import Matrix, check_gated, check_linear, gated, half_step, rows, stream_of, vectors
 
 pytestmark = pytest.mark.gpu
 
@@ -271,3 +272,26 @@ def test_results_at_places_of_any_kind(tokens, n_out, apart, skip):
     m.linear(x, add, y)
     check_linear(m, x, y, add)
     assert (space[:, :skip] == 3.0).all() and (space[:, skip + n_out:] == 3.0).all()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("tokens", [16, 64, 300])
+def test_gates_that_are_nearly_shut(tokens, dtype, act):
+    """Far below zero what a gate leaves is small, and right relative to its size.
+
+    One weight of 1 a row and one value of x, so g is exact.  With z = g or 2 sqrt(2 / pi) (g + 0.044715 g^3), act = g / (1 + e^-z).  In 32 bits z is
+    off by at most 4 2^-24 of itself, so e^z by 4 |z| 2^-24 of itself; by a product and a power of two it is off by (8 + |z|) 2^-23 more, and six
+    products and quotients by 2^-24 each.  Powers that 32 bits hold only as less than their least normal number are off by 2^-149."""
+    m = Matrix(40, 8, 32, dtype)
+    m.pairs[:, :, 0], m.pairs[:, :, 1] = 0.0, 1.0
+    x = torch.zeros((tokens, 8), dtype=m.dtype, device="cuda")
+    x[:, 0] = -torch.linspace(0.25, 91.0 if act == "silu" else 9.5, tokens, device="cuda")
+    g = x[:, 0].double().cpu().numpy()
+    z = g if act == "silu" else 2.0 * np.sqrt(2.0 / np.pi) * (g + 0.044715 * g ** 3)
+    want = g * g / (1.0 + np.exp(-z))                          # up is g too
+    u, least = half_step(m.dtype), 2.0 ** -25 if dtype == "fp16" else 2.0 ** -134
+    off = np.abs(want) * (4 * np.abs(z) * 2.0 ** -24 + (8 + np.abs(z)) * 2.0 ** -23 + 6 * 2.0 ** -24) + 2.0 ** -148 * np.abs(g)
+    got = gated(m, m, x, act).double().cpu().numpy()
+    for n in range(40):
+        assert (np.abs(got[:, n] - want) <= off * (1 + u) + u * np.abs(want) + least).all()
