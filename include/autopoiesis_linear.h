@@ -9,8 +9,9 @@
  * All pointers inside the structures are DEVICE pointers; the structures themselves are read on the host during the call.
  * All calls return an ap_status and never throw or abort, allocate nothing, keep nothing from one call for the next,
  * and run on the caller's stream (a hipStream_t; NULL is the default stream), so a stream capture records them.
- * Strides are in bytes and not negative.  What lies on the device cannot be checked by the host; whatever it holds, no kernel
- * reads or writes outside the memory that is described here.  Results do not depend on timing.
+ * Strides are in bytes and not negative; rows that a call writes do not overlap (rows that it reads may).  What lies on the
+ * device cannot be checked by the host; whatever it holds, no kernel reads or writes outside the memory that is described
+ * here.  Results do not depend on timing.
  * A workspace is device memory of at least the bytes that the call named ..._workspace gives for the same description, aligned
  * to 16 bytes (it may be NULL where that is 0), for the call alone until it has run.
  * Errors: AP_ERR_INVALID (null, zero, misaligned or contradicting arguments, an unknown type, a workspace that is too small),
@@ -72,7 +73,7 @@ ap_status ap_linear(const ap_weights *weights, const ap_vectors *x, const ap_vec
                     void *workspace, uint64_t workspace_bytes, void *stream);
 
 /* h[t][i] = act(x . gate_i) (x . up_i) in 32 bits, rounded once: the half of a feed-forward block that comes before its last
- * product.  gate and up are alike in type, group and sizes.  act: AP_SILU is g / (1 + e^-g), AP_GELU is
+ * product.  gate and up are alike in type, group and sizes; h must not overlap x.  act: AP_SILU is g / (1 + e^-g), AP_GELU is
  * g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2. */
 ap_status ap_gated_workspace(const ap_weights *gate, const ap_weights *up, uint32_t n_tokens, uint64_t *bytes);
 ap_status ap_gated(const ap_weights *gate, const ap_weights *up, const ap_vectors *x, const ap_vectors *h, uint32_t n_tokens,

@@ -27,6 +27,9 @@ ap_status take_vectors(const ap_vectors* v, uint32_t align, char** data, int64_t
     return AP_OK;
 }
 
+// Rows that are written have to be apart: what two of them write to one place would go by timing.
+bool apart(int64_t stride, uint64_t bytes, uint32_t n) { return n <= 1 || (uint64_t)stride >= bytes; }
+
 template <typename F> void for_type(uint32_t dtype, F f) { dtype == AP_BF16 ? f(bf16{}) : f(fp16{}); }
 template <typename F> void for_group(uint32_t g, F f) {
     if (g == 32) f(std::integral_constant<uint32_t, 32>{});
@@ -186,6 +189,8 @@ ap_status ap_weights_pack(const ap_weights* weights, const ap_vectors* values, v
     dim3 grid;
     const ap_status st = pack_params(weights, values, &p, &grid);
     if (st != AP_OK) return st;
+    const uint64_t codes = (uint64_t)p.w.blocks * (kBlock / 2), pairs = (uint64_t)p.w.blocks * (4 * kBlock / weights->group);
+    if (!apart(p.w.code_stride, codes, p.w.n_out) || !apart(p.w.pair_stride, pairs, p.w.n_out)) return AP_ERR_INVALID;
     for_type(weights->dtype, [&](auto e) {
         for_group(weights->group, [&](auto g) { hipLaunchKernelGGL((k_pack<decltype(e), g()>), grid, dim3(kPackThreads), 0, (hipStream_t)stream, p); });
     });
@@ -197,6 +202,7 @@ ap_status ap_weights_read(const ap_weights* weights, const ap_vectors* values, v
     dim3 grid;
     const ap_status st = pack_params(weights, values, &p, &grid);
     if (st != AP_OK) return st;
+    if (!apart(p.stride, 2ull * p.w.n_in, p.w.n_out)) return AP_ERR_INVALID;
     for_type(weights->dtype, [&](auto e) {
         for_group(weights->group, [&](auto g) { hipLaunchKernelGGL((k_unpack<decltype(e), g()>), grid, dim3(kPackThreads), 0, (hipStream_t)stream, p); });
     });
@@ -224,7 +230,7 @@ ap_status ap_linear(const ap_weights* weights, const ap_vectors* x, const ap_vec
     if (st == AP_OK) st = take_vectors(y, 2, &p.y, &p.y_stride);
     if (st == AP_OK) st = linear_plan(p.w[0], n_tokens, weights->group, false, &plan);
     if (st != AP_OK) return st;
-    if (!space_ok(workspace, workspace_bytes, plan.bytes)) return AP_ERR_INVALID;
+    if (!apart(p.y_stride, 2ull * p.w[0].n_out, n_tokens) || !space_ok(workspace, workspace_bytes, plan.bytes)) return AP_ERR_INVALID;
     if (n_tokens == 0) return AP_OK;
     p.x = xs, p.add = adds, p.n_tokens = n_tokens;
     return run_linear(p, plan, weights->dtype, weights->group, false, workspace, (hipStream_t)stream);
@@ -256,7 +262,7 @@ ap_status ap_gated(const ap_weights* gate, const ap_weights* up, const ap_vector
     if (gate->dtype != up->dtype || gate->group != up->group || p.w[0].n_out != p.w[1].n_out || p.w[0].n_in != p.w[1].n_in || act > AP_GELU) return AP_ERR_INVALID;
     st = linear_plan(p.w[0], n_tokens, gate->group, true, &plan);
     if (st != AP_OK) return st;
-    if (!space_ok(workspace, workspace_bytes, plan.bytes)) return AP_ERR_INVALID;
+    if (!apart(p.y_stride, 2ull * p.w[0].n_out, n_tokens) || !space_ok(workspace, workspace_bytes, plan.bytes)) return AP_ERR_INVALID;
     if (n_tokens == 0) return AP_OK;
     p.x = xs, p.n_tokens = n_tokens, p.act = act;
     return run_linear(p, plan, gate->dtype, gate->group, true, workspace, (hipStream_t)stream);

@@ -187,3 +187,19 @@ def test_scales_that_are_too_small(scale):
     """Below 2^-120 (times log2(e)) logits in 32 bits could be further apart than 32 bits hold, and yet both count."""
     _refused(b.AP_ERR_INVALID, b.ap_logprobs, _logits(dtype=b.AP_FP32, stride=4000), AT, scale, 5, AT, AT, AT, AT, AT, 1 << 40)
     b.ap_logprobs(_logits(n_rows=0), AT, 2.0 ** -120, 5, AT, AT, AT, AT)
+
+
+def test_rows_that_are_written_do_not_overlap():
+    """What two rows write to one place would go by timing."""
+    args = (AT, 1 << 40)
+    for stride in (0, 198):                                # of 100 outputs
+        y = _rows(stride=stride)
+        _refused(b.AP_ERR_INVALID, b.ap_linear, _weights(), _rows(), y, 3, None, *args)
+        _refused(b.AP_ERR_INVALID, b.ap_gated, _weights(), _weights(), _rows(), y, 3, b.AP_SILU, *args)
+        b.ap_linear(_weights(), _rows(), y, 0, None, *args)
+        b.ap_gated(_weights(), _weights(), _rows(), y, 0, b.AP_SILU, *args)
+    for change in (dict(code_stride=0), dict(code_stride=176), dict(pair_stride=0), dict(pair_stride=8)):
+        _refused(b.AP_ERR_INVALID, b.ap_weights_pack, _weights(**change), _rows())
+        assert b.ap_linear_workspace(_weights(**change), 3) == 0          # rows that are read may
+    for stride in (0, 512):
+        _refused(b.AP_ERR_INVALID, b.ap_weights_read, _weights(), _rows(stride=stride))
