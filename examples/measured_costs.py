@@ -4,8 +4,9 @@
 
 Runs one layer of a served model (paged cache, position rotation, attention) on the GPU at a grid of lengths, puts the measured
 times in the place of the roofline's attention term, and scores the same candidates with the roofline's cost tables and with the
-measured ones.  With --weights4 the projections, the feed-forward block and the output head are held in 4 bits and measured too.  The model is an 8B-class one (32 layers, 32 heads on 8), the trace the small synthetic one; the weights and rows
-are random, which no time here depends on.
+measured ones.  With --weights4 the projections, the feed-forward block and the output head are held in 4 bits and measured too, and
+the roofline beside them is that of the model in 4 bits.  The model is an 8B-class one (32 layers, 32 heads on 8), the trace the
+small synthetic one; the weights and rows are random, which no time here depends on.
 """
 import argparse
 import os
@@ -43,20 +44,24 @@ def main(argv=None):
     p.add_argument("--weights4", action="store_true", help="weights in 4 bits, measured too")
     p.add_argument("--candidates", type=int, default=64)
     a = p.parse_args(argv)
+    model = MODEL.copy()
+    if a.weights4:
+        model["weight_bits"] = 4
     tr = traces.make_trace(0)
     longest = int((tr.prompt_len + tr.out_len).max())
     grid = np.unique(np.concatenate([2 ** np.arange(4, int(np.log2(longest)) + 1), [longest]]))
-    decode_us, prefill_us = measured.layer_times(MODEL, tr.B, grid, grid, bits=a.bits, window=a.window, sinks=a.sinks)
+    decode_us, prefill_us = measured.layer_times(model, tr.B, grid, grid, bits=a.bits, window=a.window, sinks=a.sinks)
     print(f"one layer, {tr.B} slots, cache in {a.bits} bits: microseconds of append and attention")
     for n, d, f in zip(grid, decode_us, prefill_us):
         print(f"  {n:6d} tokens   decode step {d:9.1f}   prefill {f:9.1f}")
     w = binding.ap_workload_create(tr.arrival_us, tr.prompt_len, tr.out_len)
-    roofline = binding.ap_roofline_costs(w, len(tr.prompt_len), np.array([MODEL]), np.array([GPU]), np.array([(0, 0, 1, tr.B)], binding.GROUP_DTYPE))
+    roofline = binding.ap_roofline_costs(w, len(tr.prompt_len), np.array([model]), np.array([GPU]), np.array([(0, 0, 1, tr.B)], binding.GROUP_DTYPE))
     binding.ap_workload_destroy(w)
-    weights = measured.weight_times(MODEL, tr.B, grid) if a.weights4 else None
+    weights = measured.weight_times(model, tr.B, grid) if a.weights4 else None
     if weights:
         print(f"one layer's weights in 4 bits: decode step {weights[0]:.1f} us, prefill of {grid[-1]} tokens {weights[1][-1]:.1f}; output head {weights[2]:.1f}")
-    tables = measured.request_tables(MODEL, GPU, tr.B, tr.prompt_len, tr.out_len, grid, decode_us, grid, prefill_us, weights)
+    tables = measured.request_tables(model, GPU, tr.B, tr.prompt_len, tr.out_len, grid, decode_us, grid, prefill_us, weights)
+    print(f"the roofline's model has weights in {model['weight_bits']} bits")
     for name, t in (("roofline", roofline), ("measured", tables)):
         m = score(tr, t[:2], a.candidates)
         print(f"{name}: mean TTFT {m['sum_ttft_us'].mean() / len(tr.prompt_len) / 1e3:8.2f} ms, mean TPOT {m['sum_tpot_us'].mean() / len(tr.prompt_len) / 1e3:7.3f} ms, "

@@ -33,3 +33,20 @@ def test_measurements_that_are_refused(change, monkeypatch):
 def test_lengths_may_end_at_the_longest(monkeypatch):
     with pytest.raises(Reached):
         _tables(monkeypatch)
+
+
+@pytest.mark.parametrize("weights4", [False, True])
+def test_the_example_compares_like_with_like(monkeypatch, capsys, weights4):
+    """Times of weights in 4 bits stand beside the roofline of a model whose weights are in 4 bits, and take its terms' places."""
+    from examples import measured_costs as example
+    bits = []
+    monkeypatch.setattr(binding, "ap_workload_create", lambda *a: 1)
+    monkeypatch.setattr(binding, "ap_workload_destroy", lambda w: None)
+    monkeypatch.setattr(binding, "ap_roofline_costs", lambda w, n, models, gpus, groups: bits.append(int(models[0]["weight_bits"])) or (None, None))
+    monkeypatch.setattr(example.measured, "layer_times", lambda model, n, contexts, prompts, **k: bits.append(int(model["weight_bits"])) or (contexts, prompts))
+    monkeypatch.setattr(example.measured, "weight_times", lambda model, n, prompts: bits.append(int(model["weight_bits"])) or (1.0, prompts, 1.0))
+    monkeypatch.setattr(example.measured, "request_tables", lambda model, *a: bits.append(int(model["weight_bits"])) or (None, None))
+    monkeypatch.setattr(example, "score", lambda tr, tables, n: np.ones(n, binding.METRICS_DTYPE))
+    assert example.main(["--candidates", "2"] + ["--weights4"] * weights4) == 0
+    assert len(bits) == 3 + weights4 and set(bits) == {4 if weights4 else 16}
+    assert f"weights in {4 if weights4 else 16} bits" in capsys.readouterr().out
