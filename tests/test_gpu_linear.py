@@ -295,3 +295,28 @@ def test_gates_that_are_nearly_shut(tokens, dtype, act):
     got = gated(m, m, x, act).double().cpu().numpy()
     for n in range(40):
         assert (np.abs(got[:, n] - want) <= off * (1 + u) + u * np.abs(want) + least).all()
+
+
+# Sizes at which a call of few rows takes its inputs in parts: each of the kernel's numbers of tokens, whole and partial last blocks and
+# parts, results that go four at a time and that do not.
+PARTS = [(20, 514, 4104, 128, "bf16"), (32, 1021, 4352, 32, "fp16"), (17, 72, 6152, 64, "bf16"), (29, 332, 8192, 128, "fp16"), (48, 516, 4232, 64, "bf16"),
+         (1, 258, 16392, 128, "bf16"), (4, 65, 20480, 32, "fp16"), (5, 130, 16512, 64, "fp16"), (8, 34, 32776, 128, "bf16"), (16, 516, 16440, 32, "bf16")]
+GATED_PARTS = [(1, 514, 8200, 128, "bf16", "silu"), (4, 67, 12296, 32, "fp16", "gelu"), (8, 260, 8192, 64, "bf16", "gelu"), (13, 1030, 8320, 128, "fp16", "silu"),
+               (16, 36, 16392, 64, "fp16", "silu"), (20, 130, 8200, 32, "bf16", "gelu"), (32, 258, 8448, 128, "fp16", "silu"), (64, 66, 4104, 64, "bf16", "silu")]
+
+
+@pytest.mark.parametrize("tokens,n_out,n_in,group,dtype", PARTS)
+def test_inputs_in_parts(tokens, n_out, n_in, group, dtype):
+    m = Matrix(n_out, n_in, group, dtype, seed=tokens, apart=1)
+    assert b.ap_linear_workspace(m.describe(), tokens) >= 2 * 4 * tokens * n_out        # otherwise there are no parts here
+    x, add = rows(tokens, n_in, dtype, seed=n_in, apart=8), rows(tokens, n_out, dtype, seed=n_out, apart=3)
+    check_linear(m, x, m.linear(x))
+    check_linear(m, x, m.linear(x, add), add)
+
+
+@pytest.mark.parametrize("tokens,n_out,n_in,group,dtype,act", GATED_PARTS)
+def test_gated_inputs_in_parts(tokens, n_out, n_in, group, dtype, act):
+    gate, up = Matrix(n_out, n_in, group, dtype, seed=tokens), Matrix(n_out, n_in, group, dtype, seed=tokens + 1, apart=1)
+    assert b.ap_gated_workspace(gate.describe(), up.describe(), tokens) >= 2 * 8 * tokens * n_out
+    x = rows(tokens, n_in, dtype, seed=n_in, apart=8)
+    check_gated(gate, up, x, gated(gate, up, x, act), act)
