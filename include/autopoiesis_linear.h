@@ -65,7 +65,9 @@ ap_status ap_weights_read(const ap_weights *weights, const ap_vectors *values, v
 /* y = x W^T (+ add) for n_tokens rows: y[t][n] = add[t][n] + sum_k x[t][k] (lo + step * code)[n][k], in 32 bits with each
  * rounded once, at its end.  x (16-byte aligned) has n_in columns, y and add have n_out; all are of the weights' type.  add may
  * be NULL, or y itself; with a stride of 0 it is a bias.  y must not overlap x.  Rows are apart: what is not a number in one
- * of x reaches only the same row of y.  No weight is rounded: sums over a group's columns of x (16 + code) and of x meet
+ * of x reaches only the same row of y.  A call gives the same each time; the order in which a sum's terms are added goes by
+ * n_out, n_in, n_tokens and the output's place, so the same product in a larger matrix or among other rows can differ by
+ * roundings in 32 bits.  No weight is rounded: sums over a group's columns of x (16 + code) and of x meet
  * step and lo - 16 step in 32 bits.  Where such a sum or product passes 32 bits (x and weights of 2^120 and more) or x holds an
  * infinity the row can be NaN. */
 ap_status ap_linear_workspace(const ap_weights *weights, uint32_t n_tokens, uint64_t *bytes);

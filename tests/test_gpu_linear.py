@@ -320,3 +320,15 @@ def test_gated_inputs_in_parts(tokens, n_out, n_in, group, dtype, act):
     assert b.ap_gated_workspace(gate.describe(), up.describe(), tokens) >= 2 * 8 * tokens * n_out
     x = rows(tokens, n_in, dtype, seed=n_in, apart=8)
     check_gated(gate, up, x, gated(gate, up, x, act), act)
+
+
+@pytest.mark.parametrize("tokens", [12, 30, 60, 200])
+def test_a_share_of_the_outputs_is_the_same_within_roundings(tokens):
+    """The order in which a sum's terms are added goes by the sizes of a call and by where in the matrix an output lies: a device's share of
+    the outputs, here with more parts and fewer workgroups, is the same product, within what sums in 32 bits may be off."""
+    m = Matrix(5000, 4096 + 24, 64, "bf16", seed=71)
+    x = rows(tokens, m.n_in, "bf16", seed=72)
+    part = Matrix(340, m.n_in, 64, "bf16", seed=71)
+    part.words, part.pairs = m.words[3330:3670], m.pairs[3330:3670]
+    check_linear(part, x, part.linear(x))
+    check_linear(part, x, m.linear(x)[:, 3330:3670])
