@@ -69,7 +69,8 @@ ap_status ap_weights_read(const ap_weights *weights, const ap_vectors *values, v
  * n_out, n_in, n_tokens and the output's place, so the same product in a larger matrix or among other rows can differ by
  * roundings in 32 bits.  No weight is rounded: sums over a group's columns of x (16 + code) and of x meet
  * step and lo - 16 step in 32 bits.  Where such a sum or product passes 32 bits (x and weights of 2^120 and more) or x holds an
- * infinity the row can be NaN. */
+ * infinity the row can be NaN.  Fewer tokens can need a larger workspace than more do (their inputs are cut into more parts): one
+ * buffer for several numbers of tokens has the largest of what they need. */
 ap_status ap_linear_workspace(const ap_weights *weights, uint32_t n_tokens, uint64_t *bytes);
 ap_status ap_linear(const ap_weights *weights, const ap_vectors *x, const ap_vectors *add, const ap_vectors *y, uint32_t n_tokens,
                     void *workspace, uint64_t workspace_bytes, void *stream);

@@ -203,3 +203,11 @@ def test_rows_that_are_written_do_not_overlap():
         assert b.ap_linear_workspace(_weights(**change), 3) == 0          # rows that are read may
     for stride in (0, 512):
         _refused(b.AP_ERR_INVALID, b.ap_weights_read, _weights(), _rows(stride=stride))
+
+
+def test_a_workspace_is_for_one_number_of_tokens():
+    """Many tokens fill the chip without parts, a few hundred do not: a buffer for the most of them is refused for fewer."""
+    w, x, y = b.make_weights(b.AP_BF16, 128, 4096, 14336, AT, AT), b.make_vectors(AT, 14336), b.make_vectors(AT, 4096)
+    needs = {n: b.ap_linear_workspace(w, n) for n in (300, 8192)}
+    assert needs[8192] < needs[300]
+    _refused(b.AP_ERR_INVALID, b.ap_linear, w, x, y, 300, None, AT, needs[8192])
