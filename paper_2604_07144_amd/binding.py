@@ -455,7 +455,7 @@ def ap_weights_read(weights: ApWeights, values: ApVectors, stream: int = 0) -> N
 
 
 def ap_linear_workspace(weights: ApWeights, n_tokens: int) -> int:
-    """Bytes of device memory that ap_linear needs for so many tokens."""
+    """Bytes of device memory that ap_linear needs for just so many tokens; fewer can need more."""
     need = C.c_uint64()
     _check(lib().ap_linear_workspace(weights, n_tokens, need), "ap_linear_workspace")
     return need.value
@@ -467,6 +467,7 @@ def ap_linear(weights: ApWeights, x: ApVectors, y: ApVectors, n_tokens: int, add
 
 
 def ap_gated_workspace(gate: ApWeights, up: ApWeights, n_tokens: int) -> int:
+    """Bytes of device memory that ap_gated needs for just so many tokens; fewer can need more."""
     need = C.c_uint64()
     _check(lib().ap_gated_workspace(gate, up, n_tokens, need), "ap_gated_workspace")
     return need.value

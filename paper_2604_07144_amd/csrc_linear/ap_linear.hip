@@ -60,14 +60,19 @@ struct LinearPlan {
 
 constexpr uint32_t kCus = 256;
 
+// Times beside the choices below are us a call, of calls in a graph with weights that come from memory.
+
 // Up to kMostFew tokens go to the kernel of few rows, whose workgroup has all of them and 128 outputs or fewer; the other one's has
-// 512 outputs.  64 tokens, few / many, bf16, groups of 128, us: 4096 outputs of 4096 inputs 15.2 / 19.7, 4096 of 14336 25 / 31, 10240 of
-// 8192 31 / 34, gated 14336 of 4096 36 / 40.
+// 512 outputs.  64 tokens, few / many, bf16, groups of 128: 4096 outputs of 4096 inputs 15.2 / 19.7, 4096 of 14336 25 / 31, 10240 of 8192
+// 31 / 34, gated 14336 of 4096 36 / 40.  (Other numbers of tokens and small groups were not compared.)
 constexpr uint32_t kMostFew = 64;
 
 // Estimates of the kernel of many rows, us: what a workgroup's step of 128 columns takes besides its tiles of 16 tokens and for each
 // of them, what comes before the first and after the last step, what a second launch costs, and bytes of parts that are written and read a us.
-// (With 5 for 8, what a single tile takes now, 2048 tokens of 14336 gated outputs of 4096 get tiles of 64 for 96: 579 us for 539.)
+// Expected / measured, groups of 128: 65, 100 tokens, 4096 outputs of 4096 inputs 24 / 20, 27 / 21; 128, 14336 of 4096 44 / 36; 331, 5120 of 13824
+// 83 / 81; gated 14336 of 4096, 2048 tokens 530 / 521, 4999 1206 / 1120.  The terms are those of groups of 128: gated 14336 of 4096, 2048 tokens,
+// groups of 64 and 32, 530 / 635 and 535 / 806.  And kEnterUs is more than a single tile takes to begin and to end (5): with 5 that product, in
+// groups of 128, gets tiles of 64 for 96 and took 579 for 539; a round of workgroups that is not full, or not in step, has no term of its own.
 constexpr double kStepUs = 0.3, kTileUs = 0.46, kEnterUs = 8, kJoinUs = 4, kPartBytesPerUs = 4e6;
 
 ap_status linear_plan(const Weights& w, uint32_t n_tokens, uint32_t group, bool gated, LinearPlan* out) {
@@ -96,12 +101,13 @@ ap_status linear_plan(const Weights& w, uint32_t n_tokens, uint32_t group, bool 
         r.tokens = n_tokens <= 4 ? 4 : n_tokens <= 8 ? 8 : n_tokens <= 16 ? 16 : n_tokens <= 32 ? 32 : 64;
         const uint32_t aside = r.tokens <= 16 ? (gated ? 2 : 1) : r.tokens / 8;
         r.n_outs = tiles_of(tiles, aside), r.n_tokens = 1;
-        // With few outputs as many parts as fill the chip, of four steps each at least: 4096 outputs of 14336 inputs, 64 tokens, in 1, 3 and
-        // 8 parts 94, 41 and 26 us; 10240 of 8192 in 1, 2 and 3 56, 37 and 32 us.  Where a workgroup has few tokens it has its outputs in
+        // With few outputs as many parts as fill the chip, of four steps of 16 wavefronts each at least, which are eight of the 8 wavefronts that
+        // 5 to 16 tokens have (16 tokens, 2048 outputs of 14336 inputs stay one part, 11.0): 64 tokens, 4096 outputs of 14336 inputs in 1, 3
+        // and 8 parts 94, 41 and 26; 10240 of 8192 in 1, 2 and 3 56, 37 and 32.  Where a workgroup has few tokens it has its outputs in
         // several tiles one after another, and no more workgroups are started than there are CUs.
         parts = std::max<uint32_t>(1, std::min(kCus / std::min(kCus, r.n_outs), w.blocks * aside / 64));
         if (r.tokens <= 16) r.n_outs = std::min(r.n_outs, kCus);
-        // From three tiles on x is brought to LDS once, where it fits, and not with each.  Brought with each / once, us: gated 14336 of 4096, 1, 4
+        // From three tiles on x is brought to LDS once, where it fits, and not with each.  Brought with each / once: gated 14336 of 4096, 1, 4
         // and 8 tokens 20.3 / 18.4, 20.2 / 18.2, 23.5 / 21.4; 128256 of 4096, 8 tokens 85 / 74; two tiles (6144 of 4096), 1 and 8 tokens 6.6 / 7.1
         // and 7.6 / 7.4; one tile (4096 of 4096) 4.8 / 5.4 and 5.4 / 5.7.
         r.held = r.tokens <= 8 && (uint64_t)tiles_of(w.blocks, parts) * r.tokens * 256 <= kHeldBytes && tiles > 2ull * kCus * aside;

@@ -104,7 +104,7 @@ template <uint32_t G> using PairWords = uint32_t __attribute__((ext_vector_type(
 
 // Both are g / (1 + e^-z), with z = g, and with 2 sqrt(2 / pi) (g + 0.044715 g^3): (1 + tanh u) / 2 is 1 / (1 + e^-2u), which does not cancel.  e^-z is a
 // square and everything 2^-40 as large until it has been inverted: nothing overflows before the factor of g, a number down to 2^-149, is
-// lost for the result's type too.
+// lost for the result's type too.  (Gated 14336 of 4096, 4999 tokens 1106 us, with tanh and whole divisions 1119.)
 __device__ __forceinline__ float activated(float g, uint32_t act) {
     const float z = act == AP_SILU ? g : 1.5957691216057308f * fmaf(0.044715f * g * g, g, g), root = __builtin_amdgcn_exp2f(-0.72134752044448170f * z);
     return g * (__builtin_amdgcn_rcpf(fmaf(root * 0x1p-40f, root, 0x1p-40f)) * 0x1p-40f);

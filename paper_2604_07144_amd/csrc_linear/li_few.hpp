@@ -16,8 +16,9 @@
 //
 // What bounds it: up to 16 tokens what a CU brings to LDS, codes from memory and x and pairs from the L2 (about 9 TB/s over the chip, where
 // loads that go to registers row by row reach a third); from 32 tokens on that and the vector unit in turn, as the wavefronts that share
-// x keep step.  Measured, groups of 128, bf16, us (the bytes at the 5.1 TB/s of a copy): one token, 4096 outputs of 4096 inputs 4.9 in a
-// graph (1.7); 8 tokens, gated 14336 of 4096 20.8 (12.2), 128256 of 4096 74 (55); 64 tokens, 10240 of 8192 31 (9.1).
+// x keep step.  Measured, groups of 128, bf16, us of a graph's steps with weights that come from memory (in brackets the bytes
+// at the 5.1 TB/s of a copy): one token, 4096 outputs of 4096 inputs 4.9 (1.7); 8 tokens, gated 14336 of 4096 20 (12.2), 128256 of 4096 74 (55); 64
+// tokens, 10240 of 8192 in fp16 32 (9.1).  With weights that the chip's caches hold: the gated product 15.7, the last one 26.7.
 #ifndef LI_FEW_HPP
 #define LI_FEW_HPP
 

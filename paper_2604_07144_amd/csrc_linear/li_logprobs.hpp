@@ -1,7 +1,7 @@
 // Log probabilities of given tokens, entropy and the largest logits of rows: one pass over the logits.
 //
 // In powers of two, with c = scale log2(e) and a reference m near the largest logit:  d = (x - m) c,  S = sum 2^d,  Q = sum 2^d d,  and then
-// log2 p = d - log2 S,  entropy / ln 2 = log2 S - Q / S.  m is one number for a wavefront and is raised when a logit passes it by kRise
+// log p = scale (x - m) - log S,  entropy = log S - ln 2 Q / S.  m is one number for a wavefront and is raised when a logit passes it by kRise
 // in d, so that it is seldom raised: sums have room for terms of 2^kRise.  (x c - m c by one multiply-add would spare a subtraction,
 // but m c is rounded: a token that has all the probability would not get 0.)
 //
@@ -9,10 +9,10 @@
 // looks only at entries above the last place that is asked for.  Those are gathered in LDS and merged in when there are many.
 // Wavefronts of a row, and pieces of a row where there are few rows, are joined in order at the end.
 //
-// Measured, 128256 tokens, us: 2311 rows in bf16 with 8 alternatives 124 (4.8 TB/s; a copy 5.1); 64 rows in 32 bits with 20 alternatives
-// 19.7, 8 rows in bf16 with 5 11.9: a launch that joins (5) and finding the alternatives (64 rows without any 10), which is vector work
-// of every wavefront, sorting networks of 64 keys.  So what a wavefront has in its registers, four spans, goes into the first bound at once: by
-// the first span only, 132, 21.8 and 13.2.
+// Measured, 128256 tokens, us a call among others: 2311 rows in bf16 with 8 alternatives 124.5 (4.8 TB/s; a copy 5.1; under a kernel trace
+// 134), in 32 bits 220 (5.4 TB/s); 64 rows in 32 bits with 20 alternatives 19.5, 8 rows in bf16 with 5 12.3: a launch that joins (5) and finding
+// the alternatives (64 rows without any 10), which is vector work of every wavefront, sorting networks of 64 keys.  So what a wavefront has in its registers, four spans, goes into the first bound at once: by
+// the first span only 132 for 124, 21.8 for 19.7 and 13.2 for 11.9.
 #ifndef LI_LOGPROBS_HPP
 #define LI_LOGPROBS_HPP
 

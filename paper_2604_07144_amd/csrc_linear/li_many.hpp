@@ -6,10 +6,11 @@
 // one is worked on.  The sums X of x, which all outputs share, are taken by a wavefront for each tile of tokens.
 //
 // A tile of 16 tokens and 64 outputs is 16 products (256 cycles) and 32 multiply-adds that scale them, which the compiler puts between the
-// next tile's products.  Measured, gated 14336 outputs of 4096 inputs, bf16, TFLOP/s (a large product of the library 1130): 4999 tokens
-// 1030 with groups of 128; 2048 tokens 890 with groups of 128, 750 of 64, 592 of 32, which scale two and four times as often.  Without the
-// loads 20 % less time, without the scaling 4 %; weights two blocks ahead in a ring of three changed nothing.  Results leave four outputs a thread:
-// one at a time 300 tokens, 2048 outputs of 1024 inputs, took 20.1 us for 16.4.
+// next tile's products.  Measured, gated 14336 outputs of 4096 inputs, bf16, TFLOP/s (a large product of the library 1130 to 1160): 4999 tokens
+// 1000 to 1060 from card to card with groups of 128 (under a kernel trace 956); 2048 tokens 924 with groups of 128, 758 of 64, 597 of 32,
+// which scale two and four times as often.  Without the loads 20 % less time, without the scaling 4 %; weights two blocks ahead in a ring of
+// three changed nothing.  Results leave four outputs a thread: one at a time 300 tokens, 2048 outputs of 1024 inputs, took 20.1 us for 16.4 (14.7
+// since the parts are joined four at a time too).
 #ifndef LI_MANY_HPP
 #define LI_MANY_HPP
 

@@ -4,7 +4,7 @@
 // lanes a block, so a wavefront four of them, which may be of different rows.  The range of a group is taken over 4, 8 or 16 lanes.
 //
 // Measured, 28672 rows of 8192, groups of 64: packing 174 us (3.5 TB/s: memory and vector unit in turn; with a division for each value
-// 196), reading back 118 (5.1 TB/s, what a copy moves); 4096 of 4096 14 and 8.
+// 196), reading back 119 (5.1 TB/s, what a copy moves); 4096 of 4096 14 to 16 and 8.
 #ifndef LI_PACK_HPP
 #define LI_PACK_HPP
 
