@@ -11,8 +11,8 @@
 //
 // Measured, 128256 tokens, us a call among others: 2311 rows in bf16 with 8 alternatives 124.5 (4.8 TB/s; a copy 5.1; under a kernel trace
 // 134), in 32 bits 220 (5.4 TB/s); 64 rows in 32 bits with 20 alternatives 19.5, 8 rows in bf16 with 5 12.3: a launch that joins (5) and finding
-// the alternatives (64 rows without any 10), which is vector work of every wavefront, sorting networks of 64 keys.  So what a wavefront has in its registers, four spans, goes into the first bound at once: by
-// the first span only 132 for 124, 21.8 for 19.7 and 13.2 for 11.9.
+// the alternatives (64 rows without any 10), which is vector work of every wavefront, sorting networks of 64 keys.  So what a wavefront has in
+// its registers, four spans, goes into the first bound at once: by the first span only 132 for 124, 21.8 for 19.7 and 13.2 for 11.9.
 #ifndef LI_LOGPROBS_HPP
 #define LI_LOGPROBS_HPP
 
@@ -168,8 +168,8 @@ __device__ __forceinline__ double log_of(float s) {
 }
 
 // What a row's sums and largest logits say.  Once a row and so in 64 bits, with the scale itself: differences of logits that pass 32 bits are
-// numbers here, and beside what the sums are off there is one rounding (8 rows of 128256: 12.35 us for 12.1 in 32 bits).  The sums were taken with c, which is rounded; what that makes of
-// log S goes by the mean of d, to first order, and is put back.
+// numbers here, and beside what the sums are off there is one rounding (8 rows of 128256: 12.35 us for 12.1 in 32 bits).  The sums were taken
+// with c, which is rounded; what that makes of log S goes by the mean of d, to first order, and is put back.
 template <typename E> __device__ __forceinline__ void answer(const LogParams& p, uint32_t row, Given t, Sums x, uint64_t key, uint32_t lane) {
     if (!(x.s < INFINITY)) x.s = __builtin_nanf("");                   // an infinity that no limit in 32 bits lay below was a weight, and not no number
     const double with_c = log_of(x.s), mean = x.q / x.s * kLn2, whole = fma(p.beyond_c, mean, with_c);
